@@ -303,6 +303,114 @@ int sparse_attn_decode(int64_t pos, int32_t stride_l, int32_t summary_c, int32_t
                        size_t workspace_bytes, void* stream);
 
 /*
+ * Rotary positions of several axes (the time, row, column, channel ... of a
+ * token; the patterns of Sec. 4.3 see a sequence only): q and k are turned
+ * pairwise by angles proportional to the token's place on each axis, so that
+ * q_i . k_j depends on the differences of their places.
+ *   axis_dims[a]   elements of d_head that axis a owns: even, >= 2, axis 0 first, the
+ *                  sum at most d_head; elements behind the last axis pass unchanged
+ *   base           > 1: pair t of an axis of size s turns by place * base^(-2 t / s)
+ *   pairing        SA_ROTARY_ADJACENT: pair t of an axis is its elements 2t, 2t + 1;
+ *                  SA_ROTARY_HALVES: its elements t and t + s / 2
+ *   inverse        0: (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos); 1: by the opposite
+ *                  angles.  The rotation is orthogonal, so with inverse = 1 the call
+ *                  is the gradient: of dL/dq_out, dL/dk_out it makes dL/dq, dL/dk.
+ * q is [batch, q_heads, n, d_head] with element strides q_strides[0..2] (batch,
+ * head, token), d contiguous; q_out has the same shape and strides of its own.
+ * k, k_out alike with k_heads (keys that query heads share).  Either tensor can
+ * be absent: its heads 0, its pointers and strides ignored.  An output may be
+ * its own input (same address and strides); other overlaps are not allowed.
+ *   positions      device int32, axis fastest: token i of batch b has its place on axis
+ *                  a at positions[b * position_strides[0] + i * position_strides[1] + a]
+ *                  (position_strides[0] = 0: one set of places for the whole batch);
+ *                  any int32, negative ones included
+ *   n              1 <= n < 2^31 (n = 1: the new token of every sequence)
+ *   n_axes         1 .. 4
+ * Angles are exact to 2^-31 turns at every place; products in fp32, one rounding at
+ * the end.  Every base address 16-byte aligned and every stride of q, k and the
+ * outputs a multiple of 16 bytes, token strides >= d_head; positions 4-byte
+ * aligned, strides >= 0.  d_head in {32, 64, 128}; batch * n < 2^33, else
+ * SA_ERR_UNSUPPORTED.
+ */
+enum { SA_ROTARY_ADJACENT = 0, SA_ROTARY_HALVES = 1 };
+
+int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_heads, int32_t d_head, int32_t dtype,
+                       const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides,
+                       const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides,
+                       const int32_t* positions, const int64_t* position_strides, int32_t n_axes,
+                       const int32_t* axis_dims, double base, int32_t pairing, int32_t inverse, void* stream);
+
+/*
+ * A key / value cache in 8 bits.  Codes are e4m3 (OCP: 4 exponent bits, 3 of
+ * mantissa, up to 448, no infinity), with one fp32 scale, a power of two, for
+ * every block of scale_block tokens of one (batch, head), keys and values
+ * apart: element = code * scale.
+ *   k_cache, v_cache  [batch, kv_heads, capacity, d_head] bytes, strides
+ *                     cache_strides[0..2] in bytes (batch, head, token) for both,
+ *                     d contiguous.  Keys and values may interleave (v_cache =
+ *                     k_cache + d_head, token stride 2 d_head: a token's key and
+ *                     value lie together, which gathered tokens gain from).
+ *   k_scale, v_scale  [batch, kv_heads, ceil(capacity / scale_block)] contiguous fp32
+ *   scale_block       in {16, 32, 64, 128};  capacity in [1, 2^31 - 1]
+ *
+ * sparse_attn_cache8_store writes n_new new keys and values of every sequence
+ * (n_new = 1: one generated token), [batch, kv_heads, n_new, d_head] with element
+ * strides kv_strides[0..2] for both, d contiguous, bf16 or fp32 (dtype):
+ * sequence b's first counts[b] of them go to positions start[b], start[b] + 1, ...
+ *   start   device int32 [batch], or NULL: 0 for all.  A negative start leaves the
+ *           sequence's cache as it is.
+ *   counts  device int32 [batch], or NULL: n_new for all.  Taken as 0 below 0 and as
+ *           n_new above it; tokens that would lie at or behind `capacity` are not
+ *           stored.
+ * The scale of a block is the least power of two 2^e with every magnitude of its
+ * tokens <= 448 * 2^e, e in [-100, 120]; a code is the nearest e4m3 to x * 2^-e,
+ * ties to even.  Where start[b] lies inside a block, its earlier tokens stay:
+ * the new scale is at least the old one, and where it grows, their codes become
+ * the nearest e4m3 to code * (old scale / new scale), which is exact but for
+ * codes that turn subnormal.  Positions of the block behind the new tokens keep
+ * their bytes but not their meaning (the scale is the block's).  A NaN or an
+ * infinity is stored as NaN and has no part in the scale.
+ * SA_ERR_UNSUPPORTED for 2^24 or more blocks of new tokens in one call.
+ */
+int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int32_t d_head, int32_t dtype,
+                             const void* k, const void* v, const int64_t* kv_strides, const int32_t* start,
+                             const int32_t* counts, int64_t capacity, int32_t scale_block, void* k_cache,
+                             void* v_cache, const int64_t* cache_strides, float* k_scale, float* v_scale,
+                             void* stream);
+
+/*
+ * sparse_attn_decode over an 8-bit cache, every sequence at a position of its
+ * own: query row b is at positions[b] and attends S_positions[b] (Sec. 4.3,
+ * 5.1) over positions 0 .. positions[b] of sequence b's cache.
+ *   positions  device int32 [batch], read when the call runs (a captured call can be
+ *              replayed for later positions).  A negative one is a sequence without a
+ *              query: o = 0, lse = -inf.  One above max_pos: o and lse are NaN.
+ *   max_pos    upper bound of the positions, 0 <= max_pos < capacity: sets the launch
+ *              and the workspace (a bound far above the positions costs time only)
+ *   heads, kv_heads  kv_heads divides heads; query head h reads cache head
+ *              h / (heads / kv_heads) and attends the set of head h
+ *   q, o       [batch, heads, d_head] of type dtype, element strides q_strides[0..1]
+ *   lse        [batch, heads] contiguous fp32, natural log
+ * Cache arguments as for sparse_attn_cache8_store (scales powers of two).  Codes
+ * times scales are exact in bf16; q . k is accumulated in fp32 from unrounded
+ * terms.  Rows outside the set are never read into a result.  Every base
+ * address 16-byte aligned (scales and positions 4), cache strides multiples
+ * of 16, q strides multiples of 16 bytes, the cache's token stride >= d_head.
+ * workspace as for sparse_attn_decode, of sparse_attn_decode8_workspace_size bytes.
+ * batch * heads < 2^22, else SA_ERR_UNSUPPORTED.
+ */
+int sparse_attn_decode8_workspace_size(int64_t max_pos, int32_t stride_l, int32_t summary_c, int32_t pattern,
+                                       int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                                       int32_t d_head, int32_t dtype, size_t* bytes);
+
+int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t stride_l, int32_t summary_c,
+                        int32_t pattern, int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                        int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides, const void* k_cache,
+                        const void* v_cache, const int64_t* cache_strides, const float* k_scale,
+                        const float* v_scale, int64_t capacity, int32_t scale_block, float softmax_scale, void* o,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Strided pattern, merged heads (SA_STRIDED, SA_MODE_MERGED), with the A2
  * part computed by transposition (Sec. 5.5: reordered by residue mod l, a
  * stride of l becomes a local window), with the caller choosing the class

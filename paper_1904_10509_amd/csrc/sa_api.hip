@@ -306,6 +306,39 @@ int check_decode_shape(int32_t batch, int32_t heads, int32_t d, int32_t dtype) {
     return SA_OK;
 }
 
+// Query rows of a step over an 8-bit cache: a launch takes fewer than 2^32 threads.
+constexpr int64_t kMaxRows8 = 1 << 22;
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// Strides of whole 16-byte pieces, the last one (the rows') no less than a row.
+bool rows_ok(const int64_t* strides, int count, int64_t unit, int32_t row) {
+    for (int t = 0; t < count; ++t)
+        if (strides[t] < 0 || strides[t] % unit != 0) return false;
+    return strides[count - 1] >= row;
+}
+
+// Arguments of an 8-bit cache.
+int check_cache8(const void* k, const void* v, const int64_t* strides, const float* ks, const float* vs,
+                 int64_t capacity, int32_t scale_block, int32_t d, sa::Cache8* out) {
+    if (capacity < 1 || capacity > INT32_MAX) return SA_ERR_INVALID;
+    if (scale_block != 16 && scale_block != 32 && scale_block != 64 && scale_block != 128) return SA_ERR_INVALID;
+    if (!k || !v || !strides || !ks || !vs) return SA_ERR_INVALID;
+    if (!aligned16(k) || !aligned16(v) || !aligned4(ks) || !aligned4(vs)) return SA_ERR_INVALID;
+    if (!rows_ok(strides, 3, 16, d)) return SA_ERR_INVALID;
+    out->k = (uint8_t*)const_cast<void*>(k);
+    out->v = (uint8_t*)const_cast<void*>(v);
+    out->ks = const_cast<float*>(ks);
+    out->vs = const_cast<float*>(vs);
+    out->sb = strides[0];
+    out->sh = strides[1];
+    out->ss = strides[2];
+    out->capacity = (int32_t)capacity;
+    out->block_shift = __builtin_ctz((unsigned)scale_block);
+    out->blocks = (int32_t)((capacity + scale_block - 1) / scale_block);
+    return SA_OK;
+}
+
 // Merged strided heads by transposition through the explicit entry points:
 // the band over the caller's strided A1 layout, the classes in blocks of
 // class_block (see class_args); tensors contiguous.
@@ -635,6 +668,130 @@ int sparse_attn_decode(int64_t pos, int32_t stride_l, int32_t summary_c, int32_t
                                      dtype, q, q_strides, k_cache, v_cache, kv_strides, softmax_scale, o, lse,
                                      workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_heads, int32_t d_head, int32_t dtype,
+                       const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides,
+                       const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides,
+                       const int32_t* positions, const int64_t* position_strides, int32_t n_axes,
+                       const int32_t* axis_dims, double base, int32_t pairing, int32_t inverse, void* stream) {
+    if (batch < 1 || n < 1 || n > INT32_MAX || q_heads < 0 || k_heads < 0 || (q_heads == 0 && k_heads == 0))
+        return SA_ERR_INVALID;
+    if (dtype != SA_F32 && dtype != SA_BF16) return SA_ERR_INVALID;
+    if (d_head != 32 && d_head != 64 && d_head != 128) return SA_ERR_UNSUPPORTED;
+    if (!positions || !position_strides || !axis_dims || !aligned4(positions)) return SA_ERR_INVALID;
+    if (position_strides[0] < 0 || position_strides[1] < 0) return SA_ERR_INVALID;
+    if (n_axes < 1 || n_axes > sa::kMaxAxes) return SA_ERR_INVALID;
+    if (pairing != SA_ROTARY_ADJACENT && pairing != SA_ROTARY_HALVES) return SA_ERR_INVALID;
+    if (inverse != 0 && inverse != 1) return SA_ERR_INVALID;
+    if (!isfinite(base) || !(base > 1.0)) return SA_ERR_INVALID;
+    if ((int64_t)batch * n >= (int64_t)1 << 33) return SA_ERR_UNSUPPORTED;
+    sa::RotaryCall c;
+    c.batch = batch;
+    c.n = n;
+    c.d = d_head;
+    c.dtype = dtype;
+    const int64_t unit = dtype == SA_BF16 ? 8 : 4;  // elements per 16 bytes
+    auto tensor = [&](int32_t heads, const void* x, const int64_t* xs, void* y, const int64_t* ys, sa::RotaryTensor* t) {
+        *t = {};
+        t->heads = heads;
+        if (heads == 0) return true;
+        if (!x || !xs || !y || !ys || !aligned16(x) || !aligned16(y)) return false;
+        if (!rows_ok(xs, 3, unit, d_head) || !rows_ok(ys, 3, unit, d_head)) return false;
+        if (x == y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2])) return false;
+        t->x = x;
+        t->y = y;
+        t->xb = xs[0], t->xh = xs[1], t->xs = xs[2];
+        t->yb = ys[0], t->yh = ys[1], t->ys = ys[2];
+        return true;
+    };
+    if (!tensor(q_heads, q, q_strides, q_out, q_out_strides, &c.t[0])) return SA_ERR_INVALID;
+    if (!tensor(k_heads, k, k_strides, k_out, k_out_strides, &c.t[1])) return SA_ERR_INVALID;
+    int64_t sum = 0;
+    for (int a = 0; a < sa::kMaxAxes; ++a) c.dims[a] = 0;
+    for (int a = 0; a < n_axes; ++a) {
+        if (axis_dims[a] < 2 || axis_dims[a] % 2 != 0) return SA_ERR_INVALID;
+        c.dims[a] = axis_dims[a];
+        sum += axis_dims[a];
+    }
+    if (sum > d_head) return SA_ERR_INVALID;
+    c.places = positions;
+    c.pb = position_strides[0];
+    c.pn = position_strides[1];
+    c.axes = n_axes;
+    c.base = base;
+    c.halves = pairing == SA_ROTARY_HALVES;
+    c.inverse = inverse != 0;
+    return sa::rotary_launch(c, static_cast<hipStream_t>(stream)) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int32_t d_head, int32_t dtype,
+                             const void* k, const void* v, const int64_t* kv_strides, const int32_t* start,
+                             const int32_t* counts, int64_t capacity, int32_t scale_block, void* k_cache,
+                             void* v_cache, const int64_t* cache_strides, float* k_scale, float* v_scale,
+                             void* stream) {
+    int st = check_decode_shape(batch, kv_heads, d_head, dtype);
+    if (st != SA_OK) return st;
+    if (n_new < 1 || n_new > INT32_MAX) return SA_ERR_INVALID;
+    sa::Cache8 cache;
+    st = check_cache8(k_cache, v_cache, cache_strides, k_scale, v_scale, capacity, scale_block, d_head, &cache);
+    if (st != SA_OK) return st;
+    if (!k || !v || !kv_strides || !aligned16(k) || !aligned16(v) || !aligned4(start) || !aligned4(counts))
+        return SA_ERR_INVALID;
+    if (!rows_ok(kv_strides, 3, dtype == SA_BF16 ? 8 : 4, d_head)) return SA_ERR_INVALID;
+    // one workgroup per (batch, head, block that the new tokens can reach)
+    if (((n_new + scale_block - 2) / scale_block + 1) * batch * kv_heads >= 1 << 24) return SA_ERR_UNSUPPORTED;
+    return sa::cache8_store_launch(cache, batch, kv_heads, n_new, d_head, dtype, k, v, kv_strides, start, counts,
+                                   static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SA_OK
+               : SA_ERR_HIP;
+}
+
+int sparse_attn_decode8_workspace_size(int64_t max_pos, int32_t stride_l, int32_t summary_c, int32_t pattern,
+                                       int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                                       int32_t d_head, int32_t dtype, size_t* bytes) {
+    int32_t internal = 0, sub = 0;
+    int st = check_decode_pattern(max_pos, stride_l, summary_c, pattern, head_mode, &internal, &sub);
+    if (st != SA_OK) return st;
+    st = check_decode_shape(batch, heads, d_head, dtype);
+    if (st != SA_OK) return st;
+    if (kv_heads < 1 || heads % kv_heads != 0 || !bytes) return SA_ERR_INVALID;
+    if ((int64_t)batch * heads >= kMaxRows8) return SA_ERR_UNSUPPORTED;
+    *bytes = sa::decode8_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c, batch, heads,
+                                         kv_heads, d_head);
+    return SA_OK;
+}
+
+int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t stride_l, int32_t summary_c,
+                        int32_t pattern, int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                        int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides, const void* k_cache,
+                        const void* v_cache, const int64_t* cache_strides, const float* k_scale,
+                        const float* v_scale, int64_t capacity, int32_t scale_block, float softmax_scale, void* o,
+                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    int32_t internal = 0, sub = 0;
+    int st = check_decode_pattern(max_pos, stride_l, summary_c, pattern, head_mode, &internal, &sub);
+    if (st != SA_OK) return st;
+    st = check_decode_shape(batch, heads, d_head, dtype);
+    if (st != SA_OK) return st;
+    if (kv_heads < 1 || heads % kv_heads != 0) return SA_ERR_INVALID;
+    if ((int64_t)batch * heads >= kMaxRows8) return SA_ERR_UNSUPPORTED;
+    sa::Cache8 cache;
+    st = check_cache8(k_cache, v_cache, cache_strides, k_scale, v_scale, capacity, scale_block, d_head, &cache);
+    if (st != SA_OK) return st;
+    if (max_pos >= capacity) return SA_ERR_INVALID;
+    if (!positions || !q || !q_strides || !o || !lse) return SA_ERR_INVALID;
+    if (!aligned4(positions) || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return SA_ERR_INVALID;
+    if (!rows_ok(q_strides, 2, dtype == SA_BF16 ? 8 : 4, 0)) return SA_ERR_INVALID;
+    if (!isfinite(softmax_scale) || !(softmax_scale > 0.f)) return SA_ERR_INVALID;
+    const size_t need = sa::decode8_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c,
+                                                    batch, heads, kv_heads, d_head);
+    if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
+    if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
+    return sa::decode8_launch(cache, positions, internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c, batch,
+                              heads, kv_heads, d_head, dtype, q, q_strides, softmax_scale, o, lse, workspace,
+                              static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SA_OK
+               : SA_ERR_HIP;
 }
 
 int sparse_attn_transposed_workspace_size(int64_t n, int32_t block, int32_t stride_l, int32_t class_block,

@@ -1,0 +1,52 @@
+// e4m3 (OCP: sign, 4 exponent bits, 3 of mantissa, largest 448, 0x7f / 0xff NaN) with
+// power-of-two scales.
+//
+// Why powers of two: code * scale is exact (in bf16 as well: 4 significant bits), so is
+// x * 2^-e ahead of the one rounding, and moving a code to a larger scale is exact
+// unless it turns subnormal.  A finer scale would gain nothing: a floating format's
+// relative step is the same wherever in its range a block lies.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sa {
+
+constexpr int kMinExp = -100, kMaxExp = 120;  // of a scale
+
+// Least e with amax <= 448 * 2^e, clamped; amax as the bits of a finite float >= 0.
+// amax = m 2^x, 1 <= m < 2, and 448 = 1.75 * 2^8: e = x - 8, one more for m > 1.75.
+__host__ __device__ inline int scale_exponent(uint32_t amax) {
+    const int e = (int)(amax >> 23) - 127 - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return e < kMinExp ? kMinExp : (e > kMaxExp ? kMaxExp : e);
+}
+// The exponent of a stored scale (clamped: memory that was never stored to holds anything).
+__host__ __device__ inline int exponent_of(uint32_t scale) {
+    const int e = (int)(scale >> 23 & 0xffu) - 127;
+    return e < kMinExp ? kMinExp : (e > kMaxExp ? kMaxExp : e);
+}
+// Bits of 2^e, -126 <= e <= 127.
+__host__ __device__ inline uint32_t power_bits(int e) { return (uint32_t)(e + 127) << 23; }
+
+#ifdef __HIP_DEVICE_COMPILE__
+// Four floats of magnitude <= 448 as codes, nearest, ties to even; x[0] in the low byte.
+__device__ inline uint32_t encode4(const float* x) {
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], r, true);
+    return (uint32_t)r;
+}
+// Four codes as floats.
+__device__ inline void decode4(uint32_t u, float* x) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, false);
+    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)u, true);
+    x[0] = lo[0];
+    x[1] = lo[1];
+    x[2] = hi[0];
+    x[3] = hi[1];
+}
+#else
+__device__ inline uint32_t encode4(const float*) { return 0; }
+__device__ inline void decode4(uint32_t, float*) {}
+#endif
+
+}  // namespace sa

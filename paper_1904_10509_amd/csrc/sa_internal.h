@@ -316,6 +316,46 @@ hipError_t decode_launch(int pattern, int mode, int32_t sub, int32_t pos, int32_
                          const int64_t* kv_strides, float scale, void* o, float* lse, void* workspace,
                          hipStream_t stream);
 
+// One rotary call (sa_rotary.hip): up to two tensors turned by one set of places.
+constexpr int kMaxAxes = 4;
+struct RotaryTensor {
+    int32_t heads;                // 0: absent
+    const void* x;
+    void* y;
+    int64_t xb, xh, xs, yb, yh, ys;  // element strides: batch, head, token
+};
+struct RotaryCall {
+    int32_t batch;
+    int64_t n;
+    int32_t d, dtype;
+    RotaryTensor t[2];
+    const int32_t* places;
+    int64_t pb, pn;               // strides of the places: batch, token
+    int32_t axes, dims[kMaxAxes];
+    double base;
+    bool halves, inverse;
+};
+hipError_t rotary_launch(const RotaryCall& c, hipStream_t stream);
+
+// An 8-bit cache (sa_cache8.hip): codes with one power-of-two scale per 2^block_shift
+// tokens of a (batch, head).
+struct Cache8 {
+    uint8_t *k, *v;
+    float *ks, *vs;
+    int64_t sb, sh, ss;           // byte strides: batch, head, token
+    int32_t capacity, blocks;     // tokens; scale blocks per (batch, head)
+    int32_t block_shift;
+};
+hipError_t cache8_store_launch(const Cache8& cache, int batch, int kv_heads, int64_t n_new, int d, int dtype,
+                               const void* k, const void* v, const int64_t* kv_strides, const int32_t* start,
+                               const int32_t* counts, hipStream_t stream);
+size_t decode8_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c,
+                               int batch, int heads, int kv_heads, int d);
+hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pattern, int mode, int32_t sub,
+                          int32_t max_pos, int32_t l, int32_t c, int batch, int heads, int kv_heads, int d, int dtype,
+                          const void* q, const int64_t* q_strides, float scale, void* o, float* lse, void* workspace,
+                          hipStream_t stream);
+
 size_t bwd_workspace_bytes(int64_t batch, int64_t heads, int64_t n, int64_t nq, int n_layouts);
 
 // Launches of a backward call: the row statistics (pre), dQ, and dK / dV.

@@ -9,6 +9,7 @@ outputs with torch and calls those same entry points.
 Loading fails loudly when the library has not been built; there is no
 fallback implementation.
 """
+import contextlib
 import ctypes
 import math
 import os
@@ -26,6 +27,7 @@ SA_STRIDED, SA_FIXED, SA_FIXED_PER_HEAD = 0, 1, 2
 SA_MODE_A1, SA_MODE_A2, SA_MODE_MERGED, SA_MODE_INTERLEAVED = 0, 1, 2, 3
 SA_F32, SA_BF16 = 0, 1
 SA_TILE_FULL, SA_TILE_MASKED = 0, 1
+SA_ROTARY_ADJACENT, SA_ROTARY_HALVES = 0, 1
 SA_BWD_ROW_STATS, SA_BWD_DQ, SA_BWD_DKDV, SA_BWD_ALL_STAGES = 1, 2, 4, 7
 
 EXPORTED = (
@@ -37,6 +39,10 @@ EXPORTED = (
     "sparse_attn_bwd",
     "sparse_attn_decode_workspace_size",
     "sparse_attn_decode",
+    "sparse_attn_rotary",
+    "sparse_attn_cache8_store",
+    "sparse_attn_decode8_workspace_size",
+    "sparse_attn_decode8",
     "sparse_attn_transposed_workspace_size",
     "sparse_attn_fwd_transposed",
     "sparse_attn_bwd_transposed",
@@ -74,6 +80,12 @@ def lib():
         _DEC = [_i64, _i32, _i32, _i32, _i32]  # pos, stride_l, summary_c, pattern, head_mode
         L.sparse_attn_decode_workspace_size.argtypes = _DEC + [_i32] * 4 + [_vp]
         L.sparse_attn_decode.argtypes = _DEC + [_i32] * 4 + [_vp] * 5 + [_f32] + [_vp] * 3 + [_sz, _vp]
+        L.sparse_attn_rotary.argtypes = ([_i32, _i64] + [_i32] * 4 + [_vp] * 10 + [_i32, _vp, ctypes.c_double, _i32, _i32,
+                                                                                   _vp])
+        L.sparse_attn_cache8_store.argtypes = ([_i32, _i32, _i64, _i32, _i32] + [_vp] * 5 + [_i64, _i32] + [_vp] * 6)
+        L.sparse_attn_decode8_workspace_size.argtypes = _DEC + [_i32] * 5 + [_vp]
+        L.sparse_attn_decode8.argtypes = ([_vp] + _DEC + [_i32] * 5 + [_vp] * 7 + [_i64, _i32, _f32] + [_vp] * 3
+                                          + [_sz, _vp])
         _TR = [_i64, _i32, _i32, _i32]  # n, block, stride_l, class_block
         L.sparse_attn_transposed_workspace_size.argtypes = _TR + [_i32] * 4 + [_vp]
         L.sparse_attn_fwd_transposed.argtypes = _TR + [_vp] * 3 + [_i32] * 4 + [_vp] * 3 + [_f32] + [_vp] * 3 + [_sz, _vp]
@@ -271,6 +283,43 @@ def sparse_attn_decode(pos, stride_l, summary_c, pattern, head_mode, batch, head
     _check("sparse_attn_decode", st)
 
 
+def sparse_attn_rotary(batch, n, q_heads, k_heads, d_head, dtype, q, q_strides, q_out, q_out_strides, k, k_strides,
+                       k_out, k_out_strides, positions, position_strides, n_axes, axis_dims, base, pairing, inverse,
+                       stream=None):
+    st = lib().sparse_attn_rotary(batch, n, q_heads, k_heads, d_head, dtype, _ptr(q), q_strides, _ptr(q_out),
+                                  q_out_strides, _ptr(k), k_strides, _ptr(k_out), k_out_strides, _ptr(positions),
+                                  position_strides, n_axes, axis_dims, base, pairing, inverse,
+                                  _stream(stream, positions.device))
+    _check("sparse_attn_rotary", st)
+
+
+def sparse_attn_cache8_store(batch, kv_heads, n_new, d_head, dtype, k, v, kv_strides, start, counts, capacity,
+                             scale_block, k_cache, v_cache, cache_strides, k_scale, v_scale, stream=None):
+    st = lib().sparse_attn_cache8_store(batch, kv_heads, n_new, d_head, dtype, _ptr(k), _ptr(v), kv_strides, _ptr(start),
+                                        _ptr(counts), capacity, scale_block, _ptr(k_cache), _ptr(v_cache),
+                                        cache_strides, _ptr(k_scale), _ptr(v_scale), _stream(stream, k.device))
+    _check("sparse_attn_cache8_store", st)
+
+
+def sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads, d_head,
+                                       dtype):
+    out = ctypes.c_size_t(0)
+    st = lib().sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, batch, heads,
+                                                  kv_heads, d_head, dtype, ctypes.byref(out))
+    _check("sparse_attn_decode8_workspace_size", st)
+    return out.value
+
+
+def sparse_attn_decode8(positions, max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads, d_head,
+                        dtype, q, q_strides, k_cache, v_cache, cache_strides, k_scale, v_scale, capacity, scale_block,
+                        softmax_scale, o, lse, workspace, workspace_bytes, stream=None):
+    st = lib().sparse_attn_decode8(_ptr(positions), max_pos, stride_l, summary_c, pattern, head_mode, batch, heads,
+                                   kv_heads, d_head, dtype, _ptr(q), q_strides, _ptr(k_cache), _ptr(v_cache),
+                                   cache_strides, _ptr(k_scale), _ptr(v_scale), capacity, scale_block, softmax_scale,
+                                   _ptr(o), _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream, q.device))
+    _check("sparse_attn_decode8", st)
+
+
 # ---------------------------------------------------------------------------
 # Convenience layer: torch allocates, the entry points above compute
 # ---------------------------------------------------------------------------
@@ -394,6 +443,216 @@ def decode(q, k_cache, v_cache, pos, stride_l, summary_c, pattern, head_mode, so
         # a pattern or shape that the size query refuses is reported by it, with or without a workspace
         sparse_attn_decode_workspace_size(pos, stride_l, summary_c, pattern, head_mode, b, h, d, dtype)
         raise
+    return o, lse
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions of several axes, and the 8-bit cache with its decoding step
+# ---------------------------------------------------------------------------
+def _here(device, stream):
+    """Context in which a call's buffers are allocated and its kernels launched: the
+    tensors' device current and, where the caller names a stream, that stream too
+    (memory from another stream's pool could still be in use there)."""
+    if stream is None:
+        return _SAME if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    return torch.cuda.stream(stream)
+
+
+_SAME = contextlib.nullcontext()
+
+
+def _longs(values):
+    return (ctypes.c_int64 * len(values))(*values)
+
+
+def _row_strides(t):
+    """Strides of [batch, heads, n, d]; a dimension of one element is never stepped over, so torch's value for it is
+    replaced by one that any layout has."""
+    b, h, n, d = t.shape
+    st = t.stride()
+    return _longs((st[0] if b > 1 else 0, st[1] if h > 1 else 0, st[2] if n > 1 else d))
+
+
+def _check_ints(name, t, shape, device):
+    """A contiguous int32 tensor on the device."""
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on the device of the other tensors")
+
+
+def grid_positions(shape, device="cuda"):
+    """Places of the tokens of a grid in raster order, [tokens, axes] int32, for ``rotary``: (frames, rows, columns) of
+    a video, (rows, columns, channels) of an image, (n,) of a sequence."""
+    axes = torch.meshgrid(*(torch.arange(s, dtype=torch.int32, device=device) for s in shape), indexing="ij")
+    return torch.stack([a.reshape(-1) for a in axes], dim=1)
+
+
+def rotary(q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT, inverse=False, out=None, stream=None):
+    """q and k turned by their tokens' places on each axis: (q_out, k_out).
+
+    q [b, h, n, d] and k [b, kv_h, n, d] (k may be None), or [b, h, d] and [b, kv_h, d]
+    for one token a sequence.  ``positions``: int32 [n, axes] or [b, n, axes] (one
+    token: [b, axes]); ``axis_dims``: the elements of d that each axis owns.
+    ``inverse`` turns back, which is also the gradient.  ``out``: (q_out, k_out), the
+    inputs themselves allowed."""
+    single = q.dim() == 3
+    tensors = (q,) if k is None else (q, k)
+    for t in tensors:
+        if q.dim() not in (3, 4) or t.dim() != q.dim() or t.shape[0] != q.shape[0] or t.shape[2:] != q.shape[2:]:
+            raise ValueError("q and k must be [batch, heads, n, d] (or [batch, heads, d]) of one batch, n and d")
+    for t in tensors:
+        if t.dtype != q.dtype or t.device != q.device or t.device.type != "cuda":
+            raise ValueError("q and k must share type and GPU")
+        if t.stride(-1) != 1:
+            raise ValueError("q and k must have d contiguous")
+    b, n, d = q.shape[0], 1 if single else q.shape[2], q.shape[-1]
+    dims = [int(a) for a in axis_dims]
+    if positions.dtype != torch.int32 or positions.device != q.device:
+        raise ValueError("positions must be int32, on the device of q and k")
+    shape = tuple(positions.shape)
+    shared = not single and shape in ((n, len(dims)), (1, n, len(dims)))
+    if not shared and shape != ((b, len(dims)) if single else (b, n, len(dims))):
+        raise ValueError("positions must be [n, axes] or [batch, n, axes] (one token: [batch, axes])")
+    if len(dims) > 1 and positions.stride(-1) != 1:
+        raise ValueError("positions must have the axes contiguous")
+    places = _longs((0, positions.stride(-2)) if shared else (positions.stride(0), 0 if single else positions.stride(1)))
+    dtype = _dtype_code(q)
+
+    def strides(t):
+        return _row_strides(t.unsqueeze(2) if single else t)
+
+    with _here(q.device, stream):
+        if out is None:
+            outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in tensors)
+        else:
+            outs = tuple(out)[: len(tensors)]
+            for t, y in zip(tensors, outs):
+                if y.shape != t.shape or y.dtype != t.dtype or y.device != t.device or y.stride(-1) != 1:
+                    raise ValueError("out must match q and k in shape, type and device, d contiguous")
+        two = k is not None
+        sparse_attn_rotary(b, n, q.shape[1], k.shape[1] if two else 0, d, dtype, q, strides(q), outs[0], strides(outs[0]),
+                           k, strides(k) if two else None, outs[1] if two else None, strides(outs[1]) if two else None,
+                           positions, places, len(dims), (ctypes.c_int32 * len(dims))(*dims), float(base), pairing,
+                           1 if inverse else 0, stream)
+    return outs[0], outs[1] if two else None
+
+
+class Rotary(torch.autograd.Function):
+    """Autograd wrapper of ``rotary`` for [b, h, n, d] tensors: the gradient is the inverse rotation."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT):
+        ctx.save_for_backward(positions)
+        ctx.args = (tuple(axis_dims), base, pairing)
+        ctx.set_materialize_grads(False)
+        return rotary(q, k, positions, axis_dims, base, pairing)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        (positions,) = ctx.saved_tensors
+        # gradients can come expanded or permuted: rows have to be contiguous, in whole 16-byte pieces
+        grads = [g if g is None or _rows_ok(g) else g.contiguous() for g in (dq, dk)]
+        if grads[0] is None:
+            grads.reverse()  # rotary's k is the one that may be absent
+        if grads[0] is not None:
+            grads = list(rotary(grads[0], grads[1], positions, *ctx.args, inverse=True))
+        if dq is None:
+            grads.reverse()
+        return grads[0], grads[1], None, None, None, None
+
+
+def _rows_ok(t):
+    unit = 16 // t.element_size()
+    return (t.stride(-1) == 1 and t.stride(-2) >= t.shape[-1] and all(s % unit == 0 for s in t.stride()[:-1])
+            and t.data_ptr() % 16 == 0)
+
+
+@dataclass
+class Cache8:
+    """Keys and values in 8 bits (e4m3): k, v [b, kv_heads, capacity, d] (float8_e4m3fn or uint8) with one set of
+    strides, k_scale, v_scale [b, kv_heads, ceil(capacity / block)] float32."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    block: int
+
+    def _args(self, d, device):
+        """Batch, heads, capacity and strides, checked."""
+        k, v = self.k, self.v
+        if k.dim() != 4 or k.element_size() != 1 or v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+            raise ValueError("the cache's k and v must be 8-bit [batch, kv_heads, capacity, d] tensors of one layout")
+        if k.shape[3] != d or k.stride(3) != 1:
+            raise ValueError("the cache must have the d of the tensors, contiguous")
+        b, h, capacity, _ = k.shape
+        scales = (b, h, -(-capacity // self.block))
+        for t in (self.k_scale, self.v_scale):
+            if t.dtype != torch.float32 or t.shape != scales or not t.is_contiguous():
+                raise ValueError(f"the scales must be contiguous float32 tensors of shape {scales}")
+        for t in (k, v, self.k_scale, self.v_scale):
+            if t.device != device:
+                raise ValueError("the cache must be on the device of the other tensors")
+        return b, h, capacity, _row_strides(k)
+
+
+def build_cache8(batch, kv_heads, capacity, d, block=64, device="cuda"):
+    """An empty 8-bit cache.  A token's key and value lie side by side: the patterns that gather single tokens read
+    them in one piece."""
+    kv = torch.empty((batch, kv_heads, capacity, 2, d), dtype=torch.float8_e4m3fn, device=device)
+    scales = torch.empty((2, batch, kv_heads, -(-capacity // block)), dtype=torch.float32, device=device)
+    return Cache8(kv[..., 0, :], kv[..., 1, :], scales[0], scales[1], block)
+
+
+def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
+    """Write new keys and values [b, kv_heads, n_new, d] (or [b, kv_heads, d]: one token) into the cache, the first
+    counts[b] of sequence b at positions start[b], ... (int32 [b] on the device; None: 0, and all of them)."""
+    if k.dim() == 3:
+        k, v = k.unsqueeze(2), v.unsqueeze(2)
+    _strides(k, v)
+    b, h, n, d = k.shape
+    cb, ch, capacity, cache_strides = cache._args(d, k.device)
+    if (cb, ch) != (b, h):
+        raise ValueError("k and v must have the cache's batch and heads")
+    for name, t in (("start", start), ("counts", counts)):
+        if t is not None:
+            _check_ints(name, t, (b,), k.device)
+    with _here(k.device, stream):
+        sparse_attn_cache8_store(b, h, n, d, _dtype_code(k), k, v, _row_strides(k), start, counts, capacity, cache.block,
+                                 cache.k, cache.v, cache_strides, cache.k_scale, cache.v_scale, stream)
+
+
+def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode, max_pos=None, softmax_scale=None,
+            out=None, lse=None, workspace=None, stream=None):
+    """Output of one query a sequence (q: [b, h, d], at positions[b], int32 on the device; negative: no query) over the
+    8-bit cache.  ``max_pos``: an upper bound of the positions (default: the cache's last)."""
+    if q.dim() != 3 or q.stride(2) != 1 or q.device.type != "cuda":
+        raise ValueError("q must be [batch, heads, d] on the GPU, d contiguous")
+    b, h, d = q.shape
+    cb, kv_heads, capacity, cache_strides = cache._args(d, q.device)
+    if cb != b or h % kv_heads != 0:
+        raise ValueError("q must have the cache's batch and a multiple of its heads")
+    _check_ints("positions", positions, (b,), q.device)
+    max_pos = capacity - 1 if max_pos is None else max_pos
+    dtype = _dtype_code(q)
+    need = sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, dtype)
+    with _here(q.device, stream):
+        o = torch.empty_like(q) if out is None else out
+        if o.shape != q.shape or o.stride() != q.stride() or o.dtype != q.dtype or o.device != q.device:
+            raise ValueError("out must match q in shape, strides, type and device")
+        lse = torch.empty((b, h), dtype=torch.float32, device=q.device) if lse is None else lse
+        if lse.shape != (b, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device:
+            raise ValueError("lse must be a contiguous float32 [batch, heads] tensor on q's device")
+        if workspace is None:
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        elif workspace.device != q.device:
+            raise ValueError("workspace must be on q's device")
+        sparse_attn_decode8(positions, max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, dtype, q,
+                            _longs((q.stride(0) if b > 1 else 0, q.stride(1) if h > 1 else 0)), cache.k, cache.v, cache_strides, cache.k_scale, cache.v_scale, capacity,
+                            cache.block, _scale(softmax_scale, d), o, lse, workspace,
+                            workspace.numel() * workspace.element_size(), stream)
     return o, lse
 
 
