@@ -397,7 +397,8 @@ int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int
  * address 16-byte aligned (scales and positions 4), cache strides multiples
  * of 16, q strides multiples of 16 bytes, the cache's token stride >= d_head.
  * workspace as for sparse_attn_decode, of sparse_attn_decode8_workspace_size bytes.
- * batch * heads < 2^22, else SA_ERR_UNSUPPORTED.
+ * batch * heads < 2^22 and capacity * (the cache's token stride) < 64 GiB, else
+ * SA_ERR_UNSUPPORTED.
  */
 int sparse_attn_decode8_workspace_size(int64_t max_pos, int32_t stride_l, int32_t summary_c, int32_t pattern,
                                        int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,

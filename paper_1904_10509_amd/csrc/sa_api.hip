@@ -779,6 +779,8 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
     st = check_cache8(k_cache, v_cache, cache_strides, k_scale, v_scale, capacity, scale_block, d_head, &cache);
     if (st != SA_OK) return st;
     if (max_pos >= capacity) return SA_ERR_INVALID;
+    // rows of a (batch, head) are addressed in 16-byte pieces with 32 bits
+    if (cache.ss / 16 * capacity >= (int64_t)1 << 32) return SA_ERR_UNSUPPORTED;
     if (!positions || !q || !q_strides || !o || !lse) return SA_ERR_INVALID;
     if (!aligned4(positions) || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return SA_ERR_INVALID;
     if (!rows_ok(q_strides, 2, dtype == SA_BF16 ? 8 : 4, 0)) return SA_ERR_INVALID;

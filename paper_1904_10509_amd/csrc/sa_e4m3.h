@@ -10,6 +10,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "sa_mfma.h"
+
 namespace sa {
 
 constexpr int kMinExp = -100, kMaxExp = 120;  // of a scale
@@ -44,9 +46,23 @@ __device__ inline void decode4(uint32_t u, float* x) {
     x[2] = hi[0];
     x[3] = hi[1];
 }
+// Two codes of a word (its upper half if HI) times a power of two, as two bf16: exact.
+template <bool HI>
+__device__ inline uint32_t scaled2(uint32_t u, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, HI));
+}
 #else
 __device__ inline uint32_t encode4(const float*) { return 0; }
 __device__ inline void decode4(uint32_t, float*) {}
+template <bool HI>
+__device__ inline uint32_t scaled2(uint32_t, float) {
+    return 0;
+}
 #endif
+// Eight codes times a power of two, as eight bf16.
+__device__ inline bf16x8 scaled8(uint32_t lo, uint32_t hi, float scale) {
+    return __builtin_bit_cast(bf16x8, u32x4{scaled2<false>(lo, scale), scaled2<true>(lo, scale),
+                                            scaled2<false>(hi, scale), scaled2<true>(hi, scale)});
+}
 
 }  // namespace sa
