@@ -11,12 +11,18 @@
 // scale is an exact bf16 (one conversion instruction, two elements, scale included),
 // so bf16 matrix instructions lose nothing on K and V; a bf16 query goes in as it is,
 // an fp32 one as three bf16 pieces (24 bits).  A wave takes 32 keys at a time:
-//   S [32 keys x 16 heads] = K q^T   rows of K straight from memory as the A operand;
-//   P = exp2(S - running maximum)    the D layout of S is the B layout of P;
-//   O^T [d x 16] += V^T P            a lane holds 8 keys' bytes of D / 16 neighbouring
-//                                    elements; pairs of keys are interleaved in registers.
+//   S [32 keys x 16 heads] = K q^T   K's scales in the conversion;
+//   P = exp2(S - running maximum)    the D layout of S is the B layout of P; V's scales go
+//                                    into P, where a lane holds the weights of 8 keys;
+//   O^T [d x 16] += V^T P            transposing LDS reads give a lane 8 keys of one element.
 // One head alone uses one column of 16 and pays for it in matrix time only, which the
-// reads hide; what it would do with lanes on dot products is more than that.
+// reads hide.
+//
+// The rows travel through registers into LDS, a key's row of K and its row of V by
+// neighbouring lanes of one load: with both interleaved in memory a load reads whole
+// lines of 128 bytes and a run of keys in one piece.  Loading the matrix layouts
+// straight from memory instead, half a line for 16 scattered rows at a time, the
+// same bytes took 57.5 us against 45.6 (32 sequences of 65,536, 8 heads of 64, loads alone).
 #include <math.h>
 
 #include "sa_e4m3.h"
@@ -27,10 +33,7 @@ namespace sa {
 
 namespace {
 
-constexpr int kKeysPerSplit = 256;    // target keys per workgroup
-constexpr int kMaxWorkgroups = 4096;  // splits are capped at this over all units
 constexpr int kWaves = 4;
-constexpr int kCombineThreads = 256;
 constexpr int kCols = 16;             // query heads of a workgroup
 constexpr int kChunk = 32;            // keys of a wave and step
 
@@ -95,14 +98,56 @@ __device__ inline void query_pieces(const float* p, bf16x8* x) {
     }
 }
 
-// Row pieces of a chunk that a lane holds: D / 4 bytes of one key in each 16-key tile of K,
-// D / 16 bytes of each of its 8 keys of V; and a key's scales (lane = key, lane mod 32).
+// S_position as an index space (DecodeSet) in 32 bits: key t is lo + t within A1, and
+// with u = t - near behind it base + u + floor(u / c) * step: the summary columns (step =
+// l - c), or one multiple of l after the other (c = 1, step = -l - 1).
+struct KeySet {
+    uint32_t near, count;
+    int32_t lo, base, step;
+    bool alone;  // c = 1: floor(u / c) = u, which the division's 32 upper bits do not give
+    uint32_t m, shift;
+    __device__ KeySet(const DecodeSet& s) {
+        const bool a2 = s.part == PART_A2;
+        near = a2 ? 0 : (uint32_t)s.n1;
+        count = (uint32_t)s.count;
+        lo = s.a1_lo;
+        const bool strided = s.pattern == STRIDED;
+        base = strided ? (a2 ? s.pos : s.pos - 2 * s.l) : s.w;
+        step = strided ? -s.l - 1 : s.l - s.c;
+        alone = strided || s.c == 1;
+        m = s.dc.m;
+        shift = alone ? 0u : (uint32_t)(s.dc.shift - 32);
+    }
+    __device__ int32_t at(uint32_t t) const {
+        const int32_t u = (int32_t)(t - near);
+        const int32_t q = alone ? u : (int32_t)(__umulhi((uint32_t)u, m) >> shift);
+        return t < near ? lo + (int32_t)t : base + u + q * step;
+    }
+};
+
+// What a wave has in LDS: a chunk's rows (K, then V, of a key), their scales and their
+// places in the cache.  The pitch of 16 bytes more than a row spreads the 16 rows that a
+// read of K takes over the banks.
+template <int D>
+struct WaveLds {
+    static constexpr int kPitch = 2 * D + 16;
+    uint8_t rows[kChunk * kPitch];
+    float ks[kChunk], vs[kChunk];
+    uint32_t off[kChunk];
+};
+
+// The pieces of a chunk that a lane holds on their way to LDS, and a key's scales (lane = key, lane mod 32).
 template <int D>
 struct Rows {
-    uint32_t k[2][D / 16];
-    uint32_t v[8][D < 64 ? 1 : D / 64];
+    u32x4 x[D / 16];
     float ks, vs;
 };
+
+// Order of a wave's own LDS writes and reads across its lanes (the hardware keeps it).
+__device__ inline void wave_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 // Lane (g, r) = 16 g + r.  Key u of a chunk: row 4 g' + i of tile j for u = 8 g' + 4 j + i.
 template <int D, typename T, int NWV, bool DIRECT>
@@ -111,16 +156,23 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
                      float* __restrict__ lse) {
     constexpr int QP = sizeof(T) == 2 ? 1 : 3;   // pieces of a query
     constexpr int FK = D / 32, TV = D / 16;      // 32-deep products of K; 16-element tiles of V
-    __shared__ __align__(16) uint32_t s_off[NWV][kChunk];
-    __shared__ __align__(16) float s_ks[NWV][kChunk], s_vs[NWV][kChunk];
-    __shared__ float s_m[NWV][kCols];
-    __shared__ __align__(16) float s_acc[NWV / 2][kCols][D + 4];
-    __shared__ float s_l[NWV / 2][kCols];
+    constexpr int PR = D / 8;                    // 16-byte pieces of a key's rows
+    union Lds {
+        WaveLds<D> wave[NWV];
+        struct {
+            float acc[NWV][kCols][D + 4];
+            float l[NWV][kCols];
+        } join;
+    };
+    __shared__ __align__(16) Lds lds;
+    __shared__ float s_m[NWV][kCols], s_top[kCols];
 
     const int tid = threadIdx.x, lane = tid % 64, w = __builtin_amdgcn_readfirstlane(tid / 64), g = lane / 16, r = lane % 16;
-    int64_t id = blockIdx.x;
-    const int split = (int)(id % a.splits);
-    id /= a.splits;
+    // the same range of every unit in turn: the workgroups that run together read places far apart
+    // (ranges of one unit side by side: 52.8 us against 45.6, loads alone)
+    const uint32_t per_split = gridDim.x / a.splits;
+    const int split = (int)(blockIdx.x / per_split);
+    const uint32_t id = blockIdx.x % per_split;
     const int unit = (int)(id % a.u.units);
     const int64_t b = id / a.u.units;
     const int tile = unit % a.u.tiles, cls = unit / a.u.tiles % a.u.classes, kvh = unit / (a.u.tiles * a.u.classes);
@@ -130,12 +182,42 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
 
     const int32_t pos = a.positions[b];
     const bool live = pos >= 0 && pos <= a.max_pos && cols > 0;
-    const DecodeSet S(a.pattern, part_of_head(a.mode, h0), live ? pos : 0, a.l, a.sc,
-                      (int32_t)summary_start(a.l, a.sc, subblock_of_head(a.sub, h0)), a.dc);
-    const int64_t count = live ? S.count : 0;
-    const int64_t per = (count + a.splits - 1) / a.splits;
-    const int64_t t0 = split * per < count ? split * per : count, t1 = t0 + per < count ? t0 + per : count;
+    const KeySet S(DecodeSet(a.pattern, part_of_head(a.mode, h0), live ? pos : 0, a.l, a.sc,
+                             (int32_t)summary_start(a.l, a.sc, subblock_of_head(a.sub, h0)), a.dc));
+    const uint32_t count = live ? S.count : 0, per = (count + a.splits - 1) / a.splits;
+    const uint32_t t0 = min(split * per, count), t1 = min(t0 + per, count);
 
+    WaveLds<D>& mine = lds.wave[w];
+    // this lane's piece: of row 64 / PR * i + lane / PR in load i
+    const int piece = lane % PR;
+    const uint8_t* src = (piece < PR / 2 ? a.c.k : a.c.v) + b * a.c.sb + kvh * a.c.sh + 16 * (piece % (PR / 2));
+    const int64_t sbase = (b * a.kv_heads + kvh) * a.c.blocks;
+    const float *ksb = a.c.ks + sbase, *vsb = a.c.vs + sbase;
+
+    float m = -INFINITY, l = 0.f;  // running maximum of q . k (unscaled), this lane's part of the sum
+    f32x4 acc[TV];
+#pragma unroll
+    for (int t = 0; t < TV; ++t) acc[t] = zero4();
+
+    auto fetch = [&](uint32_t first, Rows<D>& x) {
+        // keys past the range repeat its last one (their weights become 0)
+        const int32_t j = S.at(min(first + lane % kChunk, t1 - 1));
+        mine.off[lane % kChunk] = (uint32_t)j * a.row16;
+        x.ks = ksb[j >> a.c.block_shift];
+        x.vs = vsb[j >> a.c.block_shift];
+        wave_order();
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            x.x[i] = __builtin_nontemporal_load(
+                reinterpret_cast<const u32x4*>(src + ((uint64_t)mine.off[64 / PR * i + lane / PR] << 4)));
+        wave_order();
+    };
+
+    // the first rows are on their way before the query is taken apart
+    constexpr uint32_t kStep = NWV * kChunk;
+    uint32_t first = t0 + w * kChunk;
+    Rows<D> x;
+    if (first < t1) fetch(first, x);
     bf16x8 qf[FK][QP];
 #pragma unroll
     for (int f = 0; f < FK; ++f) {
@@ -145,71 +227,25 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
         const int e = D == 32 ? 8 * g : 64 * (f / 2) + 16 * g + 8 * (f % 2);
         if (r < cols) query_pieces(q + b * a.qsb + (int64_t)(h0 + r * a.u.period) * a.qsh + e, qf[f]);
     }
-    const uint8_t* kb = a.c.k + b * a.c.sb + kvh * a.c.sh + (D == 32 ? 8 : 16) * g;
-    const uint8_t* vb = a.c.v + b * a.c.sb + kvh * a.c.sh + D / 16 * r;
-    const int64_t sbase = (b * a.kv_heads + kvh) * a.c.blocks;
-    const float *ksb = a.c.ks + sbase, *vsb = a.c.vs + sbase;
 
-    float m = -INFINITY, l = 0.f;  // running maximum of q . k (unscaled), this lane's part of the sum
-    f32x4 acc[TV];
+    auto attend = [&](uint32_t first, const Rows<D>& x) {
+        mine.ks[lane % kChunk] = x.ks;
+        mine.vs[lane % kChunk] = x.vs;
 #pragma unroll
-    for (int t = 0; t < TV; ++t) acc[t] = zero4();
-
-    auto fetch = [&](int64_t first, Rows<D>& x) {
-        // keys past the range repeat its last one (their weights become 0)
-        const int64_t u = first + lane % kChunk;
-        const int32_t j = S.at(u < t1 ? u : t1 - 1);
-        s_off[w][lane % kChunk] = (uint32_t)j * a.row16;
-        x.ks = ksb[j >> a.c.block_shift];
-        x.vs = vsb[j >> a.c.block_shift];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const uint8_t* p = kb + ((uint64_t)s_off[w][8 * (r / 4) + 4 * t + r % 4] << 4);
-            if constexpr (D == 32) {
-                const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-                x.k[t][0] = y[0];
-                x.k[t][1] = y[1];
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    const u32x4 y = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 64 * i));
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x.k[t][4 * i + e] = y[e];
-                }
-            }
-        }
-        const u32x4 o0 = *reinterpret_cast<const u32x4*>(&s_off[w][8 * g]), o1 = *reinterpret_cast<const u32x4*>(&s_off[w][8 * g + 4]);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const uint8_t* p = vb + ((uint64_t)(t < 4 ? o0[t % 4] : o1[t % 4]) << 4);
-            if constexpr (D == 32) {
-                x.v[t][0] = __builtin_nontemporal_load(reinterpret_cast<const uint16_t*>(p));
-            } else if constexpr (D == 64) {
-                x.v[t][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
-            } else {
-                const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-                x.v[t][0] = y[0];
-                x.v[t][1] = y[1];
-            }
-        }
-        __builtin_amdgcn_wave_barrier();  // the offsets are read before the next chunk's are written
-    };
-
-    auto attend = [&](int64_t first, const Rows<D>& x) {
-        s_ks[w][lane % kChunk] = x.ks;
-        s_vs[w][lane % kChunk] = x.vs;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        for (int i = 0; i < D / 16; ++i)
+            *reinterpret_cast<u32x4*>(mine.rows + (64 / PR * i + lane / PR) * WaveLds<D>::kPitch + 16 * piece) = x.x[i];
+        wave_order();
         f32x4 s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const float ks = s_ks[w][8 * (r / 4) + 4 * t + r % 4];
+            const int u = 8 * (r / 4) + 4 * t + r % 4;
+            const uint8_t* row = mine.rows + u * WaveLds<D>::kPitch;
+            const float ks = mine.ks[u];
             s[t] = zero4();
 #pragma unroll
             for (int f = 0; f < FK; ++f) {
-                const bf16x8 kf = scaled8(x.k[t][2 * f], x.k[t][2 * f + 1], ks);
+                const u32x2 k8 = *reinterpret_cast<const u32x2*>(row + (D == 32 ? 8 * g : 64 * (f / 2) + 16 * g + 8 * (f % 2)));
+                const bf16x8 kf = scaled8(k8[0], k8[1], ks);
 #pragma unroll
                 for (int i = QP - 1; i >= 0; --i) s[t] = mfma_16x16x32(kf, qf[f][i], s[t]);
             }
@@ -242,6 +278,12 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
                 s[t][i] = exp2_fast(fmaf(s[t][i], a.scale_log2, -shift));
                 l += s[t][i];
             }
+        const f32x4 v0 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g]), v1 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g + 4]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[0][i] *= v0[i];
+            s[1][i] *= v1[i];
+        }
         // weights in bf16: a bf16 result is rounded no finer than each of them; an fp32 result takes a second
         // piece for the remainder (2^-17 of a weight)
         bf16x8 hi, lo;
@@ -249,121 +291,101 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
             hi = pack_bf16x8(s[0], s[1]);
         else
             split_bf16x8(s[0], s[1], hi, lo);
-        const f32x4 v0 = *reinterpret_cast<const f32x4*>(&s_vs[w][8 * g]), v1 = *reinterpret_cast<const f32x4*>(&s_vs[w][8 * g + 4]);
 #pragma unroll
-        for (int half = 0; half < TV / 2; ++half) {  // elements 2 half, 2 half + 1 of the lane's TV
-            uint32_t pair[8];
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const float vs = t < 4 ? v0[t % 4] : v1[t % 4];
-                pair[t] = half % 2 ? scaled2<true>(x.v[t][half / 2], vs) : scaled2<false>(x.v[t][half / 2], vs);
-            }
-            u32x4 even, odd;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                even[i] = __builtin_amdgcn_perm(pair[2 * i + 1], pair[2 * i], 0x05040100);
-                odd[i] = __builtin_amdgcn_perm(pair[2 * i + 1], pair[2 * i], 0x07060302);
-            }
-            const bf16x8 fe = __builtin_bit_cast(bf16x8, even), fo = __builtin_bit_cast(bf16x8, odd);
-            acc[2 * half] = mfma_16x16x32(fe, hi, acc[2 * half]);
-            acc[2 * half + 1] = mfma_16x16x32(fo, hi, acc[2 * half + 1]);
-            if constexpr (QP != 1) {
-                acc[2 * half] = mfma_16x16x32(fe, lo, acc[2 * half]);
-                acc[2 * half + 1] = mfma_16x16x32(fo, lo, acc[2 * half + 1]);
-            }
+        for (int t = 0; t < TV; ++t) {
+            // lane i of a row of 16 gets element 16 t + i of keys 8 g .. 8 g + 7
+            const u32x2 v8 = ld_tr8(mine.rows + (8 * g + r / 2) * WaveLds<D>::kPitch + D + 16 * t + 8 * (r % 2));
+            const bf16x8 vf = scaled8(v8[0], v8[1], 1.f);
+            acc[t] = mfma_16x16x32(vf, hi, acc[t]);
+            if constexpr (QP != 1) acc[t] = mfma_16x16x32(vf, lo, acc[t]);
         }
-        __builtin_amdgcn_wave_barrier();  // the scales are read before the next chunk's are written
+        wave_order();  // read before the next chunk is written
     };
 
-    // the next chunk's rows are on their way while a chunk is worked on
-    constexpr int64_t kStep = (int64_t)NWV * kChunk;
-    int64_t first = t0 + (int64_t)w * kChunk;
     if (first < t1) {
-        Rows<D> x, y;
-        fetch(first, x);
-        while (true) {
-            const bool more = first + kStep < t1;
-            if (more) fetch(first + kStep, y);
-            attend(first, x);
-            if (!more) break;
-            first += kStep;
-            const bool again = first + kStep < t1;
-            if (again) fetch(first + kStep, x);
-            attend(first, y);
-            if (!again) break;
-            first += kStep;
+        if constexpr (D == 128) {
+            // one chunk in registers: 4 KB more a wave on their way cost more in waves (a quarter of them) than they
+            // gained (8 sequences, 4 cache heads, 8 query heads each: 23.4 -> 20.4 us)
+            while (true) {
+                attend(first, x);
+                first += kStep;
+                if (first >= t1) break;
+                fetch(first, x);
+            }
+        } else {  // the next chunk's rows are on their way while a chunk is worked on
+            Rows<D> y;
+            while (true) {
+                const bool more = first + kStep < t1;
+                if (more) fetch(first + kStep, y);
+                attend(first, x);
+                if (!more) break;
+                first += kStep;
+                const bool again = first + kStep < t1;
+                if (again) fetch(first + kStep, x);
+                attend(first, y);
+                if (!again) break;
+                first += kStep;
+            }
         }
     }
     l = sum_over_g(l);
 
-    // join the waves: the common maximum, then sums in a fixed tree
+    // join the waves: the common maximum, then sums in the order of the waves; element
+    // 16 t + 4 g + i of head column r is acc[t][i]
     if (g == 0) s_m[w][r] = m;
     __syncthreads();
     float top = s_m[0][r];
 #pragma unroll
     for (int v = 1; v < NWV; ++v) top = fmaxf(top, s_m[v][r]);
     const float wt = weight(m, top, a.scale_log2);
-    l *= wt;
+    if (r < cols) {
 #pragma unroll
-    for (int t = 0; t < TV; ++t)
+        for (int t = 0; t < TV; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[t][i] *= wt;
-    // element TV (4 g + i) + t of head column r is acc[t][i]
-#pragma unroll
-    for (int half = NWV / 2; half >= 1; half /= 2) {
-        if (w >= half && w < 2 * half) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int t = 0; t < TV; ++t) s_acc[w - half][r][TV * (4 * g + i) + t] = acc[t][i];
-            if (g == 0) s_l[w - half][r] = l;
+            for (int i = 0; i < 4; ++i) acc[t][i] *= wt;
+            *reinterpret_cast<f32x4*>(&lds.join.acc[w][r][16 * t + 4 * g]) = acc[t];
         }
-        __syncthreads();
-        if (w < half) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int t = 0; t < TV; ++t) acc[t][i] += s_acc[w][r][TV * (4 * g + i) + t];
-            l += s_l[w][r];
+        if (g == 0) {
+            lds.join.l[w][r] = l * wt;
+            if (w == 0) s_top[r] = top * a.scale_log2;
         }
-        __syncthreads();
     }
-    if (w != 0 || r >= cols) return;
-    const int64_t head = h0 + r * a.u.period, row = b * a.heads + head;
-    if constexpr (DIRECT) {
-        T* dst = o + b * a.qsb + head * a.qsh;
-        const bool beyond = pos > a.max_pos;  // no position of this call: NaN; no key: o = 0, lse = -inf
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+    __syncthreads();
+    const bool beyond = pos > a.max_pos;  // no position of this call: NaN; no key: o = 0, lse = -inf
+    for (int i = tid; i < cols * D; i += NWV * 64) {
+        const int c = i / D, e = i % D;
+        float sum = 0.f, total = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int t = 0; t < TV; ++t) {
-                if (beyond) put_nan(dst + TV * (4 * g + i) + t);
-                else put(dst + TV * (4 * g + i) + t, acc[t][i] * inv);
-            }
-        if (g == 0) {
-            if (beyond) put_nan(lse + row);
-            else lse[row] = l > 0.f ? (top * a.scale_log2 + __log2f(l)) / kLog2e : -INFINITY;
+        for (int v = 0; v < NWV; ++v) {
+            sum += lds.join.acc[v][c][e];
+            total += lds.join.l[v][c];
         }
-    } else {
-        float* dst = part + (row * a.splits + split) * (D + 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int t = 0; t < TV; ++t) dst[TV * (4 * g + i) + t] = acc[t][i];
-        if (g == 0) {
-            dst[D] = top * a.scale_log2;
-            dst[D + 1] = l;
+        const int64_t head = h0 + c * a.u.period, row = b * a.heads + head;
+        if constexpr (DIRECT) {
+            T* dst = o + b * a.qsb + head * a.qsh + e;
+            if (beyond) put_nan(dst);
+            else put(dst, sum * (total > 0.f ? 1.f / total : 0.f));
+            if (e == 0) {
+                if (beyond) put_nan(lse + row);
+                else lse[row] = total > 0.f ? (s_top[c] + __log2f(total)) / kLog2e : -INFINITY;
+            }
+        } else {
+            float* dst = part + (row * a.splits + split) * (D + 2);
+            dst[e] = sum;
+            if (e == 0) {
+                dst[D] = s_top[c];
+                dst[D + 1] = total;
+            }
         }
     }
 }
 
 // One workgroup per (batch, head): maximum first, one lane per range; then groups of D
 // threads take every G-th range, and their sums are added in group order.
-template <int D, typename T>
-__global__ void __launch_bounds__(kCombineThreads)
+template <int D, typename T, int NT>
+__global__ void __launch_bounds__(NT)
 decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restrict__ o, float* __restrict__ lse) {
-    constexpr int G = kCombineThreads / D;
+    constexpr int G = NT / D;
     __shared__ float s_x[G][D], s_l[G];
     const int64_t row = blockIdx.x, b = row / a.heads, h = row % a.heads;
     const int tid = threadIdx.x, g = tid / D, e = tid % D;
@@ -409,14 +431,29 @@ hipError_t launch(const Decode8Args& a, int batch, const void* q, void* o, float
         return hipGetLastError();
     }
     hipLaunchKernelGGL((decode8_split_kernel<D, T, kWaves, false>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o, lse);
-    hipLaunchKernelGGL((decode8_combine_kernel<D, T>), dim3((unsigned)(batch * a.heads)), dim3(kCombineThreads), 0, stream,
-                       a, (const float*)part, (T*)o, lse);
+    const dim3 rows((unsigned)(batch * a.heads));
+    if (a.splits > 16)
+        hipLaunchKernelGGL((decode8_combine_kernel<D, T, 1024>), rows, dim3(1024), 0, stream, a, (const float*)part, (T*)o, lse);
+    else
+        hipLaunchKernelGGL((decode8_combine_kernel<D, T, 256>), rows, dim3(256), 0, stream, a, (const float*)part, (T*)o, lse);
     return hipGetLastError();
 }
 
-// Ranges per unit: about kKeysPerSplit keys each for the largest set that a
-// position up to max_pos can have, at most kMaxWorkgroups workgroups in all.
-int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t units) {
+// Ranges per unit, for the largest set that a position up to max_pos can have.
+//   One range up to 256 keys, two chunks a wave: there is nothing to join (8 heads of 64, 206 keys: one
+//   launch 4.8 us, two ranges 6.7).
+//   Else at least 128 keys a range, one chunk a wave: the fewer serial steps the better, while
+//   there are few workgroups (8 cache heads of 64, 736 keys: 256 keys a range 7.6 us, 128
+//   7.2; d = 128 fp32, 2,272 keys 11.3 | 9.4).
+//   From 512 workgroups on (1,024 for d <= 64, whose waves have less on their way) longer
+//   ranges instead, as every range costs the join (8 sequences, 4 cache heads, d = 128, 8,416
+//   keys: 2,112 workgroups 25.2, 1,024 20.4, 512 18.9), and at most 128 ranges a unit (one unit, 65,760 keys:
+//   512 ranges 15.1 us, 128 11.6).
+//   At most 1,024 keys a range (512 for d <= 64) while that makes no more than 4,096 results to join, or 512 a
+//   row: walks of different speed need more than one round (256 units of d = 128, 8,416
+//   keys: ranges of 4,208 keys 102 us, 1,052 92.5; 248 of d = 64 and about 8,200 keys: 910 48.7, 512 46.6).
+int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t units, int64_t rows,
+              int d) {
     const DivL dc = make_divl(c > 0 ? c : 1);
     // the largest set is max_pos's or (fixed) that of the last position of the l-block before
     const int32_t before = max_pos / l * l - 1;
@@ -428,10 +465,10 @@ int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, in
             count = S.count > count ? S.count : count;
         }
     }
-    int64_t splits = (count + kKeysPerSplit - 1) / kKeysPerSplit;
-    const int64_t cap = kMaxWorkgroups / units;
-    if (splits > cap) splits = cap;
-    return splits < 1 ? 1 : (int)splits;
+    if (count <= 256) return 1;
+    const int64_t few = min64(min64((count + 127) / 128, (d == 128 ? 512 : 1024) / units), 128);
+    const int64_t many = min64(min64(d == 128 ? (count + 1023) / 1024 : (count + 511) / 512, 4096 / rows), 512);
+    return (int)max64(max64(few, many), 1);
 }
 
 }  // namespace
@@ -439,7 +476,8 @@ int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, in
 size_t decode8_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c,
                                int batch, int heads, int kv_heads, int d) {
     const int64_t units = (int64_t)batch * head_units(mode, sub, heads, kv_heads).units;
-    return (size_t)batch * heads * splits_of(pattern, mode, sub, max_pos, l, c, units) * (d + 2) * sizeof(float);
+    const int64_t rows = (int64_t)batch * heads;
+    return (size_t)rows * splits_of(pattern, mode, sub, max_pos, l, c, units, rows, d) * (d + 2) * sizeof(float);
 }
 
 hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pattern, int mode, int32_t sub,
@@ -455,7 +493,7 @@ hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pat
     a.kv_heads = kv_heads;
     a.row16 = (uint32_t)(cache.ss / 16);
     a.u = head_units(mode, sub, heads, kv_heads);
-    a.splits = splits_of(pattern, mode, sub, max_pos, l, c, (int64_t)batch * a.u.units);
+    a.splits = splits_of(pattern, mode, sub, max_pos, l, c, (int64_t)batch * a.u.units, (int64_t)batch * heads, d);
     a.sub = sub;
     a.max_pos = max_pos;
     a.l = l;

@@ -120,4 +120,14 @@ __device__ inline u32x2 ld_tr16(const uint16_t* lds_ptr) {
     return __builtin_bit_cast(u32x2, v);
 }
 
+// The same of 8-bit elements (ds_read_b64_tr_b8): output lane i receives byte i mod 8 of
+// the 8 bytes addressed by input lane 2u + i/8, as its byte u (u = 0..7).  So if lane L
+// of the row points at &T[row0 + L/2][col0 + 8 (L mod 2)] of a row-major tile of bytes,
+// lane i receives T[row0 + u][col0 + i] for u = 0..7.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+__device__ inline u32x2 ld_tr8(const uint8_t* lds_ptr) {
+    i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) i32x2*)(lds_ptr));
+    return __builtin_bit_cast(u32x2, v);
+}
+
 }  // namespace sa
