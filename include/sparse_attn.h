@@ -329,8 +329,8 @@ int sparse_attn_decode(int64_t pos, int32_t stride_l, int32_t summary_c, int32_t
  * Angles are exact to 2^-31 turns at every place; products in fp32, one rounding at
  * the end.  Every base address 16-byte aligned and every stride of q, k and the
  * outputs a multiple of 16 bytes, token strides >= d_head; positions 4-byte
- * aligned, strides >= 0.  d_head in {32, 64, 128}; batch * n < 2^33, else
- * SA_ERR_UNSUPPORTED.
+ * aligned, strides >= 0.  d_head in {32, 64, 128}; batch * n < 2^33 and at most
+ * 65,535 heads of each tensor, else SA_ERR_UNSUPPORTED.
  */
 enum { SA_ROTARY_ADJACENT = 0, SA_ROTARY_HALVES = 1 };
 
@@ -370,7 +370,7 @@ int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_head
  * codes that turn subnormal.  Positions of the block behind the new tokens keep
  * their bytes but not their meaning (the scale is the block's).  A NaN or an
  * infinity is stored as NaN and has no part in the scale.
- * SA_ERR_UNSUPPORTED for 2^24 or more blocks of new tokens in one call.
+ * SA_ERR_UNSUPPORTED for 2^22 or more blocks of new tokens (all heads) in one call.
  */
 int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int32_t d_head, int32_t dtype,
                              const void* k, const void* v, const int64_t* kv_strides, const int32_t* start,

@@ -685,7 +685,7 @@ int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_head
     if (pairing != SA_ROTARY_ADJACENT && pairing != SA_ROTARY_HALVES) return SA_ERR_INVALID;
     if (inverse != 0 && inverse != 1) return SA_ERR_INVALID;
     if (!isfinite(base) || !(base > 1.0)) return SA_ERR_INVALID;
-    if ((int64_t)batch * n >= (int64_t)1 << 33) return SA_ERR_UNSUPPORTED;
+    if ((int64_t)batch * n >= (int64_t)1 << 33 || q_heads > 65535 || k_heads > 65535) return SA_ERR_UNSUPPORTED;
     sa::RotaryCall c;
     c.batch = batch;
     c.n = n;
@@ -739,8 +739,8 @@ int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int
     if (!k || !v || !kv_strides || !aligned16(k) || !aligned16(v) || !aligned4(start) || !aligned4(counts))
         return SA_ERR_INVALID;
     if (!rows_ok(kv_strides, 3, dtype == SA_BF16 ? 8 : 4, d_head)) return SA_ERR_INVALID;
-    // one workgroup per (batch, head, block that the new tokens can reach)
-    if (((n_new + scale_block - 2) / scale_block + 1) * batch * kv_heads >= 1 << 24) return SA_ERR_UNSUPPORTED;
+    // one workgroup per (batch, head, block that the new tokens can reach); a launch takes fewer than 2^32 threads
+    if (((n_new + scale_block - 2) / scale_block + 1) * batch * kv_heads >= 1 << 22) return SA_ERR_UNSUPPORTED;
     return sa::cache8_store_launch(cache, batch, kv_heads, n_new, d_head, dtype, k, v, kv_strides, start, counts,
                                    static_cast<hipStream_t>(stream)) == hipSuccess
                ? SA_OK

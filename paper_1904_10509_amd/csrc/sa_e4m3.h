@@ -46,6 +46,23 @@ __device__ inline void decode4(uint32_t u, float* x) {
     x[2] = hi[0];
     x[3] = hi[1];
 }
+// Four elements over a power of two as codes, nearest, ties to even, straight from words
+// of two bf16 or from floats; the first element in the low byte.  Magnitudes of at most
+// 448 scales.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ inline uint32_t encode_word(uint32_t ab, uint32_t cd, float scale) {
+    s16x2 r{0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, ab), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, cd), scale, true);
+    return __builtin_bit_cast(uint32_t, r);
+}
+__device__ inline uint32_t encode_word(uint32_t a, uint32_t b, uint32_t c, uint32_t d, float scale) {
+    s16x2 r{0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __uint_as_float(a), __uint_as_float(b), scale, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, __uint_as_float(c), __uint_as_float(d), scale, true);
+    return __builtin_bit_cast(uint32_t, r);
+}
 // Two codes of a word (its upper half if HI) times a power of two, as two bf16: exact.
 template <bool HI>
 __device__ inline uint32_t scaled2(uint32_t u, float scale) {
@@ -54,6 +71,8 @@ __device__ inline uint32_t scaled2(uint32_t u, float scale) {
 #else
 __device__ inline uint32_t encode4(const float*) { return 0; }
 __device__ inline void decode4(uint32_t, float*) {}
+__device__ inline uint32_t encode_word(uint32_t, uint32_t, float) { return 0; }
+__device__ inline uint32_t encode_word(uint32_t, uint32_t, uint32_t, uint32_t, float) { return 0; }
 template <bool HI>
 __device__ inline uint32_t scaled2(uint32_t, float) {
     return 0;

@@ -5,8 +5,7 @@
 // f = base^(-2 t / s) for pair t of an axis of s elements.  The gradient is the
 // rotation by -p f.  Nothing is reused but the angles, which all heads of a token
 // share: the work is bound by reading and writing q and k once.  A thread owns W
-// pairs of one token, takes their sines and cosines once, and walks heads with
-// them.
+// pairs of one token and makes their sines and cosines once for several heads.
 //
 // The angle in turns is p f / (2 pi) modulo 1.  With F = f / (2 pi) in units of
 // 2^-64 turns, the low 64 bits of the integer product p F are that fraction, with
@@ -23,6 +22,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int64_t kMaxBlocksX = 1 << 20;
+// Heads that a thread turns, all of their loads on their way at once: up to 8 of bf16, 4 of
+// fp32 (64 registers at the widest), fewer while there are not kEnoughBlocks workgroups
+// (2 sequences of 12,288, 2 x 8 heads of 64, both directions: 4 heads a thread 46.4 us, 8
+// 43.8; fp32, 3 x 4,185 tokens, 16 heads of 128: 4 heads 85.6, 12 in three rounds 92.5; one
+// token: 1 head 2.8, 8 5.5).
+template <typename T>
+constexpr int kBatch = 16 / sizeof(T);
+constexpr int64_t kEnoughBlocks = 2048;
 
 struct RotaryArgs {
     RotaryTensor t[2];
@@ -30,121 +37,125 @@ struct RotaryArgs {
     int64_t pb, pn;
     int64_t n, tokens;        // tokens of a sequence; of the call
     int32_t unit_shift;       // log2 of the units of a token
-    int32_t heads_per_slice;  // heads that a thread walks
-    int32_t rotated;          // elements that axes own
-    int32_t axes, dims[kMaxAxes];
+    int32_t heads_per_slice;  // heads that a thread turns
+    int32_t slices0;          // slices of the first tensor; the second one's follow
+    int32_t axes, rotated;    // axes; elements that they own
+    int32_t end[kMaxAxes];    // element behind each axis (behind the last one: d)
     float sign;
     uint64_t turn[64];        // F of every pair
 };
 
-template <int N>
-__device__ inline void load(const float* p, float* x) {
-    typedef float V __attribute__((ext_vector_type(N)));
-    const V v = *reinterpret_cast<const V*>(p);
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = v[e];
+template <typename T, int N>
+struct Piece {
+    typedef T type __attribute__((ext_vector_type(N)));
+};
+template <typename T>
+struct Piece<T, 1> {
+    typedef T type;
+};
+template <typename T, int N>
+__device__ inline float element(const typename Piece<T, N>::type& v, int e) {
+    if constexpr (N == 1) return (float)v;
+    else return (float)v[e];
 }
-template <>
-__device__ inline void load<1>(const float* p, float* x) {
-    *x = *p;
+template <typename T, int N>
+__device__ inline void set_element(typename Piece<T, N>::type& v, int e, float x) {
+    if constexpr (N == 1) v = (T)x;
+    else v[e] = (T)x;
 }
-template <int N>
-__device__ inline void load(const __bf16* p, float* x) {
-    typedef __bf16 V __attribute__((ext_vector_type(N)));
-    const V v = *reinterpret_cast<const V*>(p);
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (float)v[e];
+
+// Sine and cosine of an angle in units of 2^-32 turns.  fp32 results take the library's
+// (2^-23); for bf16 results, which round to 2^-8, the hardware's instructions, whose argument
+// is in turns.
+__device__ inline void turn_sincos(int32_t turn, float* s, float* c, const float*) {
+    sincospif((float)turn * 0x1p-31f, s, c);
 }
-template <>
-__device__ inline void load<1>(const __bf16* p, float* x) {
-    *x = (float)*p;
-}
-template <int N, typename T>
-__device__ inline void store(T* p, const float* x) {
-    if constexpr (N == 1) {
-        *p = (T)*x;
-    } else {
-        typedef T V __attribute__((ext_vector_type(N)));
-        V v;
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = (T)x[e];
-        *reinterpret_cast<V*>(p) = v;
-    }
+__device__ inline void turn_sincos(int32_t turn, float* s, float* c, const __bf16*) {
+    const float x = (float)turn * 0x1p-32f;
+    *s = __builtin_amdgcn_sinf(x);
+    *c = __builtin_amdgcn_cosf(x);
 }
 
 // HALVES: the W pairs are elements e0 .. e0 + W - 1 and the same half an axis further;
 // else the 2 W elements from e0 on, pair by pair.
 template <typename T, int W, bool HALVES>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
+    constexpr int N = HALVES ? W : 2 * W, P = HALVES ? 2 : 1;  // elements of a piece; pieces of a unit
+    typedef typename Piece<T, N>::type V;
     const int64_t idx = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x;
     const int64_t tok = idx >> a.unit_shift;
     if (tok >= a.tokens) return;
     const int pair = ((int)idx & ((1 << a.unit_shift) - 1)) * W;  // the unit's first pair
-    const int64_t b = tok < a.n ? 0 : tok / a.n, i = tok - b * a.n;
+    int64_t b = 0;
+    if (tok >= a.n) b = a.tokens < ((int64_t)1 << 32) ? (uint32_t)tok / (uint32_t)a.n : tok / a.n;
+    const int64_t i = tok - b * a.n;
 
-    // the axis of each pair (units of HALVES lie inside one axis), and where the unit's elements are
+    // where the unit's elements are (a unit of HALVES lies inside one axis or behind them);
+    // axes are told apart by comparisons: an index into the arguments would be one more
+    // read of memory on the way
+    int e0 = 2 * pair, half = 0;
+    if constexpr (HALVES) {
+        int at = 0, size = a.end[0];
+#pragma unroll
+        for (int x = 0; x < kMaxAxes; ++x)
+            if (2 * pair >= a.end[x]) {
+                at = a.end[x];
+                size = (x + 1 < kMaxAxes ? a.end[x + 1] : 2 * (W << a.unit_shift)) - at;
+            }
+        half = size / 2;
+        e0 = pair + at / 2;
+    }
+    auto axis_of = [&](int p) {
+        int x = 0;
+#pragma unroll
+        for (int k = 0; k < kMaxAxes; ++k) x += 2 * p >= a.end[k];
+        return x < a.axes ? x : a.axes - 1;
+    };
+
+    // the heads' elements are on their way while the angles are made
+    const bool second = (int)blockIdx.z >= a.slices0;
+    const RotaryTensor r = second ? a.t[1] : a.t[0];
+    const int h0 = ((int)blockIdx.z - (second ? a.slices0 : 0)) * a.heads_per_slice;
+    const int h1 = h0 + a.heads_per_slice < r.heads ? h0 + a.heads_per_slice : r.heads;
+    const T* x = (const T*)r.x + b * r.xb + i * r.xs + e0;
+    T* y = (T*)r.y + b * r.yb + i * r.ys + e0;
+    constexpr int B = kBatch<T>;
+    V v[B][P];
+#pragma unroll
+    for (int u = 0; u < B; ++u)
+        if (h0 + u < h1) {
+#pragma unroll
+            for (int k = 0; k < P; ++k) v[u][k] = *reinterpret_cast<const V*>(x + (h0 + u) * r.xh + k * half);
+        }
+
     const int32_t* place = a.places + b * a.pb + i * a.pn;
     float c[W], s[W];
-    int e0 = 2 * pair, half = 0;
-    bool turned = true;
-    if constexpr (HALVES) {
-        int at = 0, axis = 0;
-        while (axis < a.axes && 2 * pair >= at + a.dims[axis]) at += a.dims[axis++];
-        turned = axis < a.axes;
-        half = (turned ? a.dims[axis] : 2 * (W << a.unit_shift) - at) / 2;
-        e0 = pair + at / 2;
-        const int64_t p = turned ? place[axis] : 0;
+    const bool turned = 2 * pair < a.rotated;
+    int64_t p = place[axis_of(pair)];
 #pragma unroll
-        for (int t = 0; t < W; ++t) {
-            const int32_t f = (int32_t)(((uint64_t)p * a.turn[pair + t]) >> 32);
-            sincospif((float)f * 0x1p-31f, &s[t], &c[t]);
-        }
-    } else {
-        int at = 0, axis = 0;
-#pragma unroll
-        for (int t = 0; t < W; ++t) {
-            while (axis < a.axes && 2 * (pair + t) >= at + a.dims[axis]) at += a.dims[axis++];
-            const int64_t p = axis < a.axes ? place[axis] : 0;
-            const int32_t f = (int32_t)(((uint64_t)p * a.turn[pair + t]) >> 32);
-            sincospif((float)f * 0x1p-31f, &s[t], &c[t]);
-        }
+    for (int t = 0; t < W; ++t) {
+        if (!HALVES && t > 0) p = place[axis_of(pair + t)];
+        turn_sincos((int32_t)(((uint64_t)p * a.turn[pair + t]) >> 32), &s[t], &c[t], (const T*)nullptr);
     }
 #pragma unroll
     for (int t = 0; t < W; ++t) s[t] *= a.sign;
 
-    const int h0 = blockIdx.z * a.heads_per_slice, all = a.t[0].heads + a.t[1].heads;
-    const int h1 = h0 + a.heads_per_slice < all ? h0 + a.heads_per_slice : all;
-    for (int h = h0; h < h1; ++h) {
-        const bool second = h >= a.t[0].heads;
-        const RotaryTensor& r = a.t[second];
-        const int hh = second ? h - a.t[0].heads : h;
-        const T* x = (const T*)r.x + b * r.xb + hh * r.xh + i * r.xs + e0;
-        T* y = (T*)r.y + b * r.yb + hh * r.yh + i * r.ys + e0;
-        if constexpr (HALVES) {
-            float x0[W], x1[W], y0[W], y1[W];
-            load<W>(x, x0);
-            load<W>(x + half, x1);
+#pragma unroll
+    for (int u = 0; u < B; ++u)
+        if (h0 + u < h1) {
 #pragma unroll
             for (int t = 0; t < W; ++t) {
-                y0[t] = turned ? x0[t] * c[t] - x1[t] * s[t] : x0[t];
-                y1[t] = turned ? x0[t] * s[t] + x1[t] * c[t] : x1[t];
-            }
-            store<W>(y, y0);
-            store<W>(y + half, y1);
-        } else {
-            float v[2 * W];
-            load<2 * W>(x, v);
-#pragma unroll
-            for (int t = 0; t < W; ++t) {
-                const float x0 = v[2 * t], x1 = v[2 * t + 1];
-                if (2 * (pair + t) < a.rotated) {
-                    v[2 * t] = x0 * c[t] - x1 * s[t];
-                    v[2 * t + 1] = x0 * s[t] + x1 * c[t];
+                V &z0 = v[u][0], &z1 = v[u][P - 1];
+                const int i0 = HALVES ? t : 2 * t, i1 = HALVES ? t : 2 * t + 1;
+                const float x0 = element<T, N>(z0, i0), x1 = element<T, N>(z1, i1);
+                if (HALVES ? turned : 2 * (pair + t) < a.rotated) {
+                    set_element<T, N>(z0, i0, x0 * c[t] - x1 * s[t]);
+                    set_element<T, N>(z1, i1, x0 * s[t] + x1 * c[t]);
                 }
             }
-            store<2 * W>(y, v);
+#pragma unroll
+            for (int k = 0; k < P; ++k) *reinterpret_cast<V*>(y + (h0 + u) * r.yh + k * half) = v[u][k];
         }
-    }
 }
 
 template <typename T, int W, bool HALVES>
@@ -154,19 +165,25 @@ hipError_t launch(RotaryArgs& a, const RotaryCall& c, hipStream_t stream) {
     const int64_t blocks = (a.tokens * units + kThreads - 1) / kThreads;
     // a launch takes fewer than 2^32 threads along x
     const unsigned gx = (unsigned)(blocks < kMaxBlocksX ? blocks : kMaxBlocksX), gy = (unsigned)((blocks + gx - 1) / gx);
-    const int all = a.t[0].heads + a.t[1].heads;
-    a.heads_per_slice = all;
-    hipLaunchKernelGGL((rotary_kernel<T, W, HALVES>), dim3(gx, gy), dim3(kThreads), 0, stream, a);
+    auto slices = [&](int t) { return (a.t[t].heads + a.heads_per_slice - 1) / a.heads_per_slice; };
+    a.heads_per_slice = kBatch<T>;
+    while (a.heads_per_slice > 1 && blocks * (slices(0) + slices(1)) < kEnoughBlocks) a.heads_per_slice /= 2;
+    a.slices0 = slices(0);
+    hipLaunchKernelGGL((rotary_kernel<T, W, HALVES>), dim3(gx, gy, (unsigned)(a.slices0 + slices(1))), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
-template <typename T, bool HALVES>
+// Pieces of at most 16 bytes, so that a lane's piece follows its neighbour's; for halves
+// the widest that every axis' half is a multiple of (w, a power of two).
+template <typename T>
 hipError_t launch_width(RotaryArgs& a, const RotaryCall& c, int w, hipStream_t stream) {
+    if (!c.halves) return launch<T, 8 / sizeof(T), false>(a, c, stream);
+    if constexpr (sizeof(T) == 2)
+        if (w == 8) return launch<T, 8, true>(a, c, stream);
     switch (w) {
-    case 8: return launch<T, 8, HALVES>(a, c, stream);
-    case 4: return launch<T, 4, HALVES>(a, c, stream);
-    case 2: return launch<T, 2, HALVES>(a, c, stream);
-    default: return launch<T, 1, HALVES>(a, c, stream);
+    case 1: return launch<T, 1, true>(a, c, stream);
+    case 2: return launch<T, 2, true>(a, c, stream);
+    default: return launch<T, 4, true>(a, c, stream);
     }
 }
 
@@ -187,20 +204,17 @@ hipError_t rotary_launch(const RotaryCall& c, hipStream_t stream) {
     // of 2^-64 off at the last of 64 pairs.  No turn of a whole pair reaches 2^64: f <= 1.
     int pair = 0;
     int w = 8;
-    for (int x = 0; x < kMaxAxes; ++x) {
-        a.dims[x] = x < c.axes ? c.dims[x] : 0;
-        if (x >= c.axes) continue;
+    for (int x = 0; x < c.axes; ++x) {
         const long double step = powl((long double)c.base, -2.0L / c.dims[x]);
         long double f = 0x1p64L / 6.283185307179586476925286766559L;
         for (int t = 0; t < c.dims[x] / 2; ++t, f *= step) a.turn[pair++] = (uint64_t)(f + 0.5L);
+        a.end[x] = 2 * pair;
         while ((c.dims[x] / 2) % w != 0) w /= 2;
     }
+    for (int x = c.axes; x < kMaxAxes; ++x) a.end[x] = c.d;
     a.rotated = 2 * pair;
     while (pair < 64) a.turn[pair++] = 0;
-    if (!c.halves) w = 4;  // 8 neighbouring elements
-    if (c.dtype == 1)
-        return c.halves ? launch_width<__bf16, true>(a, c, w, stream) : launch_width<__bf16, false>(a, c, w, stream);
-    return c.halves ? launch_width<float, true>(a, c, w, stream) : launch_width<float, false>(a, c, w, stream);
+    return c.dtype == 1 ? launch_width<__bf16>(a, c, w, stream) : launch_width<float>(a, c, w, stream);
 }
 
 }  // namespace sa

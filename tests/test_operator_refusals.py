@@ -50,7 +50,7 @@ ROTARY = dict(batch=2, n=8, qh=4, kh=2, d=64, dtype=sa.SA_BF16, q=FAKE, qs=longs
     (dict(axes=0), INV), (dict(axes=5), INV), (dict(dims=ints(31, 32)), INV), (dict(dims=ints(0, 32)), INV),
     (dict(dims=ints(34, 32)), INV), (dict(dims=None), INV), (dict(base=1.0), INV), (dict(base=float("nan")), INV),
     (dict(base=float("inf")), INV), (dict(pairing=2), INV), (dict(inverse=2), INV),
-    (dict(batch=2 ** 30, n=2 ** 10), UNS),
+    (dict(batch=2 ** 30, n=2 ** 10), UNS), (dict(qh=65536), UNS), (dict(kh=2 ** 31 - 1), UNS),
 ])
 def test_rotary_refusals(L, over, expect):
     assert L.sparse_attn_rotary(*dict(ROTARY, **over).values()) == expect
