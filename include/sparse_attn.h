@@ -328,7 +328,7 @@ int sparse_attn_decode(int64_t pos, int32_t stride_l, int32_t summary_c, int32_t
  *   n_axes         1 .. 4
  * Angles are exact to 2^-31 turns at every place; products in fp32, one rounding at
  * the end.  Every base address 16-byte aligned and every stride of q, k and the
- * outputs a multiple of 16 bytes, token strides >= d_head; positions 4-byte
+ * outputs a multiple of 16 bytes, token strides >= d_head, rows of an output apart; positions 4-byte
  * aligned, strides >= 0.  d_head in {32, 64, 128}; batch * n < 2^33 and at most
  * 65,535 heads of each tensor, else SA_ERR_UNSUPPORTED.
  */
@@ -369,7 +369,8 @@ int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_head
  * the nearest e4m3 to code * (old scale / new scale), which is exact but for
  * codes that turn subnormal.  Positions of the block behind the new tokens keep
  * their bytes but not their meaning (the scale is the block's).  A NaN or an
- * infinity is stored as NaN and has no part in the scale.
+ * infinity is stored as NaN and has no part in the scale.  Rows of different
+ * sequences and heads of the cache must not overlap.
  * SA_ERR_UNSUPPORTED for 2^22 or more blocks of new tokens (all heads) in one call.
  */
 int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int32_t d_head, int32_t dtype,
@@ -390,12 +391,14 @@ int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int
  *   heads, kv_heads  kv_heads divides heads; query head h reads cache head
  *              h / (heads / kv_heads) and attends the set of head h
  *   q, o       [batch, heads, d_head] of type dtype, element strides q_strides[0..1]
+ *              and o_strides[0..1] (batch, head), d contiguous; o's rows must not overlap
  *   lse        [batch, heads] contiguous fp32, natural log
  * Cache arguments as for sparse_attn_cache8_store (scales powers of two).  Codes
  * times scales are exact in bf16; q . k is accumulated in fp32 from unrounded
  * terms.  Rows outside the set are never read into a result.  Every base
  * address 16-byte aligned (scales and positions 4), cache strides multiples
- * of 16, q strides multiples of 16 bytes, the cache's token stride >= d_head.
+ * of 16, strides of q and o multiples of 16 bytes, the cache's token stride >=
+ * d_head.  Sequences or heads may share rows of the cache (a stride of 0).
  * workspace as for sparse_attn_decode, of sparse_attn_decode8_workspace_size bytes.
  * batch * heads < 2^22 and capacity * (the cache's token stride) < 64 GiB, else
  * SA_ERR_UNSUPPORTED.
@@ -409,7 +412,7 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
                         int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides, const void* k_cache,
                         const void* v_cache, const int64_t* cache_strides, const float* k_scale,
                         const float* v_scale, int64_t capacity, int32_t scale_block, float softmax_scale, void* o,
-                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
+                        const int64_t* o_strides, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Strided pattern, merged heads (SA_STRIDED, SA_MODE_MERGED), with the A2

@@ -318,6 +318,11 @@ bool rows_ok(const int64_t* strides, int count, int64_t unit, int32_t row) {
     return strides[count - 1] >= row;
 }
 
+// Rows that are written: batches and heads that exist do not share them.
+bool rows_apart(const int64_t* strides, int32_t batch, int32_t heads, int32_t row) {
+    return (batch == 1 || strides[0] >= row) && (heads == 1 || strides[1] >= row);
+}
+
 // Arguments of an 8-bit cache.
 int check_cache8(const void* k, const void* v, const int64_t* strides, const float* ks, const float* vs,
                  int64_t capacity, int32_t scale_block, int32_t d, sa::Cache8* out) {
@@ -698,6 +703,7 @@ int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_head
         if (heads == 0) return true;
         if (!x || !xs || !y || !ys || !aligned16(x) || !aligned16(y)) return false;
         if (!rows_ok(xs, 3, unit, d_head) || !rows_ok(ys, 3, unit, d_head)) return false;
+        if (!rows_apart(ys, batch, heads, d_head)) return false;
         if (x == y && (xs[0] != ys[0] || xs[1] != ys[1] || xs[2] != ys[2])) return false;
         t->x = x;
         t->y = y;
@@ -736,6 +742,7 @@ int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int
     sa::Cache8 cache;
     st = check_cache8(k_cache, v_cache, cache_strides, k_scale, v_scale, capacity, scale_block, d_head, &cache);
     if (st != SA_OK) return st;
+    if (!rows_apart(cache_strides, batch, kv_heads, d_head)) return SA_ERR_INVALID;
     if (!k || !v || !kv_strides || !aligned16(k) || !aligned16(v) || !aligned4(start) || !aligned4(counts))
         return SA_ERR_INVALID;
     if (!rows_ok(kv_strides, 3, dtype == SA_BF16 ? 8 : 4, d_head)) return SA_ERR_INVALID;
@@ -767,7 +774,7 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
                         int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides, const void* k_cache,
                         const void* v_cache, const int64_t* cache_strides, const float* k_scale,
                         const float* v_scale, int64_t capacity, int32_t scale_block, float softmax_scale, void* o,
-                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+                        const int64_t* o_strides, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     int32_t internal = 0, sub = 0;
     int st = check_decode_pattern(max_pos, stride_l, summary_c, pattern, head_mode, &internal, &sub);
     if (st != SA_OK) return st;
@@ -781,16 +788,18 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
     if (max_pos >= capacity) return SA_ERR_INVALID;
     // rows of a (batch, head) are addressed in 16-byte pieces with 32 bits
     if (cache.ss / 16 * capacity >= (int64_t)1 << 32) return SA_ERR_UNSUPPORTED;
-    if (!positions || !q || !q_strides || !o || !lse) return SA_ERR_INVALID;
+    if (!positions || !q || !q_strides || !o || !o_strides || !lse) return SA_ERR_INVALID;
     if (!aligned4(positions) || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return SA_ERR_INVALID;
-    if (!rows_ok(q_strides, 2, dtype == SA_BF16 ? 8 : 4, 0)) return SA_ERR_INVALID;
+    const int64_t unit = dtype == SA_BF16 ? 8 : 4;  // elements per 16 bytes
+    if (!rows_ok(q_strides, 2, unit, 0) || !rows_ok(o_strides, 2, unit, 0)) return SA_ERR_INVALID;
+    if (!rows_apart(o_strides, batch, heads, d_head)) return SA_ERR_INVALID;
     if (!isfinite(softmax_scale) || !(softmax_scale > 0.f)) return SA_ERR_INVALID;
     const size_t need = sa::decode8_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c,
                                                     batch, heads, kv_heads, d_head);
     if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
     if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
     return sa::decode8_launch(cache, positions, internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c, batch,
-                              heads, kv_heads, d_head, dtype, q, q_strides, softmax_scale, o, lse, workspace,
+                              heads, kv_heads, d_head, dtype, q, q_strides, softmax_scale, o, o_strides, lse, workspace,
                               static_cast<hipStream_t>(stream)) == hipSuccess
                ? SA_OK
                : SA_ERR_HIP;

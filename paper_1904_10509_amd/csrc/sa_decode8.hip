@@ -63,7 +63,7 @@ struct Decode8Args {
     HeadUnits u;
     int32_t sub, max_pos, l, sc;
     DivL dc;
-    int64_t qsb, qsh;
+    int64_t qsb, qsh, osb, osh;  // strides of q and o
     float scale_log2;
 };
 
@@ -362,7 +362,7 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
         }
         const int64_t head = h0 + c * a.u.period, row = b * a.heads + head;
         if constexpr (DIRECT) {
-            T* dst = o + b * a.qsb + head * a.qsh + e;
+            T* dst = o + b * a.osb + head * a.osh + e;
             if (beyond) put_nan(dst);
             else put(dst, sum * (total > 0.f ? 1.f / total : 0.f));
             if (e == 0) {
@@ -412,7 +412,7 @@ decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restr
             x += s_x[t][tid];
             l += s_l[t];
         }
-        T* dst = o + b * a.qsb + h * a.qsh + tid;
+        T* dst = o + b * a.osb + h * a.osh + tid;
         if (a.positions[b] > a.max_pos) {  // no position of this call
             put_nan(dst);
             if (tid == 0) put_nan(lse + row);
@@ -447,11 +447,13 @@ hipError_t launch(const Decode8Args& a, int batch, const void* q, void* o, float
 //   7.2; d = 128 fp32, 2,272 keys 11.3 | 9.4).
 //   From 512 workgroups on (1,024 for d <= 64, whose waves have less on their way) longer
 //   ranges instead, as every range costs the join (8 sequences, 4 cache heads, d = 128, 8,416
-//   keys: 2,112 workgroups 25.2, 1,024 20.4, 512 18.9), and at most 128 ranges a unit (one unit, 65,760 keys:
-//   512 ranges 15.1 us, 128 11.6).
-//   At most 1,024 keys a range (512 for d <= 64) while that makes no more than 4,096 results to join, or 512 a
-//   row: walks of different speed need more than one round (256 units of d = 128, 8,416
-//   keys: ranges of 4,208 keys 102 us, 1,052 92.5; 248 of d = 64 and about 8,200 keys: 910 48.7, 512 46.6).
+//   keys: 2,112 workgroups 25.2, 1,024 20.4, 512 18.9), and at most 128 ranges a unit (one unit,
+//   65,760 keys: 512 ranges 15.1 us, 128 11.6).
+//   Where that leaves more than 2,048 keys a range, ranges of about 1,024 (512 for d <= 64): walks of
+//   different speed even out over more than one round (256 units of d = 128, 8,416 keys: 2 ranges
+//   102 us, 8 92.5; 248 of d = 64, about 8,200 keys: 4 48.2, 16 46.6), up to 4,096 results to join or 512
+//   a row, and whole rounds of the 1,024 workgroups that run at once (128 units of d = 64, 8,416 keys:
+//   17 ranges 32.5, 8 29.2).
 int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t units, int64_t rows,
               int d) {
     const DivL dc = make_divl(c > 0 ? c : 1);
@@ -466,9 +468,12 @@ int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, in
         }
     }
     if (count <= 256) return 1;
-    const int64_t few = min64(min64((count + 127) / 128, (d == 128 ? 512 : 1024) / units), 128);
-    const int64_t many = min64(min64(d == 128 ? (count + 1023) / 1024 : (count + 511) / 512, 4096 / rows), 512);
-    return (int)max64(max64(few, many), 1);
+    const int64_t few = max64(min64(min64((count + 127) / 128, (d == 128 ? 512 : 1024) / units), 128), 1);
+    if (count <= 2048 * few) return (int)few;
+    int64_t many = min64(min64(count / (d == 128 ? 1024 : 512), 4096 / rows), 512);
+    const int64_t rounds = units * many / 1024;
+    if (rounds > 0) many = rounds * 1024 / units;
+    return (int)max64(few, many);
 }
 
 }  // namespace
@@ -482,8 +487,8 @@ size_t decode8_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_p
 
 hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pattern, int mode, int32_t sub,
                           int32_t max_pos, int32_t l, int32_t c, int batch, int heads, int kv_heads, int d, int dtype,
-                          const void* q, const int64_t* q_strides, float scale, void* o, float* lse, void* workspace,
-                          hipStream_t stream) {
+                          const void* q, const int64_t* q_strides, float scale, void* o, const int64_t* o_strides,
+                          float* lse, void* workspace, hipStream_t stream) {
     Decode8Args a;
     a.c = cache;
     a.positions = positions;
@@ -501,6 +506,8 @@ hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pat
     a.dc = make_divl(c > 0 ? c : 1);
     a.qsb = q_strides[0];
     a.qsh = q_strides[1];
+    a.osb = o_strides[0];
+    a.osh = o_strides[1];
     a.scale_log2 = scale * kLog2eHost;
     float* part = static_cast<float*>(workspace);
     if (dtype == 1) {

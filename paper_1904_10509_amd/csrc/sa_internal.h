@@ -353,8 +353,8 @@ size_t decode8_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_p
                                int batch, int heads, int kv_heads, int d);
 hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pattern, int mode, int32_t sub,
                           int32_t max_pos, int32_t l, int32_t c, int batch, int heads, int kv_heads, int d, int dtype,
-                          const void* q, const int64_t* q_strides, float scale, void* o, float* lse, void* workspace,
-                          hipStream_t stream);
+                          const void* q, const int64_t* q_strides, float scale, void* o, const int64_t* o_strides,
+                          float* lse, void* workspace, hipStream_t stream);
 
 size_t bwd_workspace_bytes(int64_t batch, int64_t heads, int64_t n, int64_t nq, int n_layouts);
 

@@ -84,7 +84,7 @@ def lib():
                                                                                    _vp])
         L.sparse_attn_cache8_store.argtypes = ([_i32, _i32, _i64, _i32, _i32] + [_vp] * 5 + [_i64, _i32] + [_vp] * 6)
         L.sparse_attn_decode8_workspace_size.argtypes = _DEC + [_i32] * 5 + [_vp]
-        L.sparse_attn_decode8.argtypes = ([_vp] + _DEC + [_i32] * 5 + [_vp] * 7 + [_i64, _i32, _f32] + [_vp] * 3
+        L.sparse_attn_decode8.argtypes = ([_vp] + _DEC + [_i32] * 5 + [_vp] * 7 + [_i64, _i32, _f32] + [_vp] * 4
                                           + [_sz, _vp])
         _TR = [_i64, _i32, _i32, _i32]  # n, block, stride_l, class_block
         L.sparse_attn_transposed_workspace_size.argtypes = _TR + [_i32] * 4 + [_vp]
@@ -312,11 +312,12 @@ def sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, he
 
 def sparse_attn_decode8(positions, max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads, d_head,
                         dtype, q, q_strides, k_cache, v_cache, cache_strides, k_scale, v_scale, capacity, scale_block,
-                        softmax_scale, o, lse, workspace, workspace_bytes, stream=None):
+                        softmax_scale, o, o_strides, lse, workspace, workspace_bytes, stream=None):
     st = lib().sparse_attn_decode8(_ptr(positions), max_pos, stride_l, summary_c, pattern, head_mode, batch, heads,
                                    kv_heads, d_head, dtype, _ptr(q), q_strides, _ptr(k_cache), _ptr(v_cache),
                                    cache_strides, _ptr(k_scale), _ptr(v_scale), capacity, scale_block, softmax_scale,
-                                   _ptr(o), _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream, q.device))
+                                   _ptr(o), o_strides, _ptr(lse), _ptr(workspace), workspace_bytes,
+                                   _stream(stream, q.device))
     _check("sparse_attn_decode8", st)
 
 
@@ -449,6 +450,11 @@ def decode(q, k_cache, v_cache, pos, stride_l, summary_c, pattern, head_mode, so
 # ---------------------------------------------------------------------------
 # Rotary positions of several axes, and the 8-bit cache with its decoding step
 # ---------------------------------------------------------------------------
+_SAME = contextlib.nullcontext()
+_I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+_DTYPE_CODES = {torch.bfloat16: SA_BF16, torch.float32: SA_F32}
+
+
 def _here(device, stream):
     """Context in which a call's buffers are allocated and its kernels launched: the
     tensors' device current and, where the caller names a stream, that stream too
@@ -460,25 +466,17 @@ def _here(device, stream):
     return torch.cuda.stream(stream)
 
 
-_SAME = contextlib.nullcontext()
+def _row_strides(shape, st):
+    """Strides of [batch, heads, n, d] (or [batch, heads, d], one token) as the entry points take them.  A dimension of
+    one element is never stepped over, so torch's value for it is replaced by one that any layout has."""
+    return _I64x3(st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0,
+                  st[2] if len(shape) == 4 and shape[2] > 1 else shape[-1])
 
 
-def _longs(values):
-    return (ctypes.c_int64 * len(values))(*values)
-
-
-def _row_strides(t):
-    """Strides of [batch, heads, n, d]; a dimension of one element is never stepped over, so torch's value for it is
-    replaced by one that any layout has."""
-    b, h, n, d = t.shape
-    st = t.stride()
-    return _longs((st[0] if b > 1 else 0, st[1] if h > 1 else 0, st[2] if n > 1 else d))
-
-
-def _check_ints(name, t, shape, device):
-    """A contiguous int32 tensor on the device."""
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)}")
+def _check_ints(name, t, count, device):
+    """A contiguous int32 tensor of `count` elements on the device."""
+    if t.dtype != torch.int32 or t.shape != (count,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape ({count},)")
     if t.device != device:
         raise ValueError(f"{name} must be on the device of the other tensors")
 
@@ -498,57 +496,55 @@ def rotary(q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT,
     token: [b, axes]); ``axis_dims``: the elements of d that each axis owns.
     ``inverse`` turns back, which is also the gradient.  ``out``: (q_out, k_out), the
     inputs themselves allowed."""
-    single = q.dim() == 3
-    tensors = (q,) if k is None else (q, k)
-    for t in tensors:
-        if q.dim() not in (3, 4) or t.dim() != q.dim() or t.shape[0] != q.shape[0] or t.shape[2:] != q.shape[2:]:
-            raise ValueError("q and k must be [batch, heads, n, d] (or [batch, heads, d]) of one batch, n and d")
-    for t in tensors:
-        if t.dtype != q.dtype or t.device != q.device or t.device.type != "cuda":
-            raise ValueError("q and k must share type and GPU")
-        if t.stride(-1) != 1:
-            raise ValueError("q and k must have d contiguous")
-    b, n, d = q.shape[0], 1 if single else q.shape[2], q.shape[-1]
-    dims = [int(a) for a in axis_dims]
-    if positions.dtype != torch.int32 or positions.device != q.device:
-        raise ValueError("positions must be int32, on the device of q and k")
-    shape = tuple(positions.shape)
-    shared = not single and shape in ((n, len(dims)), (1, n, len(dims)))
-    if not shared and shape != ((b, len(dims)) if single else (b, n, len(dims))):
+    shape, device, dtype = q.shape, q.device, q.dtype
+    k_shape = shape if k is None else k.shape
+    # (every attribute of a tensor is a call into torch: each is read once)
+    if len(shape) not in (3, 4) or len(k_shape) != len(shape) or k_shape[0] != shape[0] or k_shape[2:] != shape[2:]:
+        raise ValueError("q and k must be [batch, heads, n, d] (or [batch, heads, d]) of one batch, n and d")
+    if device.type != "cuda" or dtype not in _DTYPE_CODES or k is not None and (k.device != device or k.dtype != dtype):
+        raise ValueError("q and k must share type and GPU, in bfloat16 or float32")
+    q_st, k_st = q.stride(), q.stride() if k is None else k.stride()
+    if q_st[-1] != 1 or k_st[-1] != 1:
+        raise ValueError("q and k must have d contiguous")
+    single = len(shape) == 3
+    b, n, d = shape[0], 1 if single else shape[2], shape[-1]
+    axes = len(axis_dims)
+    places, p_st = positions.shape, positions.stride()
+    shared = not single and places in ((n, axes), (1, n, axes))
+    if not shared and places != ((b, axes) if single else (b, n, axes)):
         raise ValueError("positions must be [n, axes] or [batch, n, axes] (one token: [batch, axes])")
-    if len(dims) > 1 and positions.stride(-1) != 1:
-        raise ValueError("positions must have the axes contiguous")
-    places = _longs((0, positions.stride(-2)) if shared else (positions.stride(0), 0 if single else positions.stride(1)))
-    dtype = _dtype_code(q)
-
-    def strides(t):
-        return _row_strides(t.unsqueeze(2) if single else t)
-
-    with _here(q.device, stream):
+    if positions.dtype != torch.int32 or positions.device != device or axes > 1 and p_st[-1] != 1:
+        raise ValueError("positions must be int32 with the axes contiguous, on the device of q and k")
+    with _here(device, stream):
         if out is None:
-            outs = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in tensors)
+            q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
         else:
-            outs = tuple(out)[: len(tensors)]
-            for t, y in zip(tensors, outs):
-                if y.shape != t.shape or y.dtype != t.dtype or y.device != t.device or y.stride(-1) != 1:
+            q_out, k_out = out[0], None if k is None else out[1]
+            for t, y in ((q, q_out), (k, k_out)):
+                if t is not None and (y.shape != t.shape or y.dtype != dtype or y.device != device or y.stride(-1) != 1):
                     raise ValueError("out must match q and k in shape, type and device, d contiguous")
-        two = k is not None
-        sparse_attn_rotary(b, n, q.shape[1], k.shape[1] if two else 0, d, dtype, q, strides(q), outs[0], strides(outs[0]),
-                           k, strides(k) if two else None, outs[1] if two else None, strides(outs[1]) if two else None,
-                           positions, places, len(dims), (ctypes.c_int32 * len(dims))(*dims), float(base), pairing,
-                           1 if inverse else 0, stream)
-    return outs[0], outs[1] if two else None
+        # (the library itself, as in store8 and decode8: the entry points above would ask every argument for its address again)
+        st = lib().sparse_attn_rotary(
+            b, n, shape[1], 0 if k is None else k_shape[1], d, _DTYPE_CODES[dtype], q.data_ptr(), _row_strides(shape, q_st),
+            q_out.data_ptr(), _row_strides(shape, q_out.stride()), None if k is None else k.data_ptr(),
+            _row_strides(k_shape, k_st), None if k is None else k_out.data_ptr(),
+            None if k is None else _row_strides(k_shape, k_out.stride()), positions.data_ptr(),
+            _I64x2(0, p_st[-2]) if shared else _I64x2(p_st[0], 0 if single else p_st[1]), axes,
+            (ctypes.c_int32 * axes)(*axis_dims), base, pairing, 1 if inverse else 0, _stream(stream, device))
+    _check("sparse_attn_rotary", st)
+    return q_out, k_out
 
 
 class Rotary(torch.autograd.Function):
-    """Autograd wrapper of ``rotary`` for [b, h, n, d] tensors: the gradient is the inverse rotation."""
+    """Autograd wrapper of ``rotary`` for [b, h, n, d] tensors.  The gradient is the inverse rotation, and its own
+    gradient the rotation again."""
 
     @staticmethod
-    def forward(ctx, q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT):
+    def forward(ctx, q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT, inverse=False):
         ctx.save_for_backward(positions)
-        ctx.args = (tuple(axis_dims), base, pairing)
+        ctx.args = (tuple(axis_dims), base, pairing, not inverse)
         ctx.set_materialize_grads(False)
-        return rotary(q, k, positions, axis_dims, base, pairing)
+        return rotary(q, k, positions, axis_dims, base, pairing, inverse)
 
     @staticmethod
     def backward(ctx, dq, dk):
@@ -558,16 +554,19 @@ class Rotary(torch.autograd.Function):
         if grads[0] is None:
             grads.reverse()  # rotary's k is the one that may be absent
         if grads[0] is not None:
-            grads = list(rotary(grads[0], grads[1], positions, *ctx.args, inverse=True))
+            turn = Rotary.apply if torch.is_grad_enabled() else rotary
+            grads = list(turn(grads[0], grads[1], positions, *ctx.args))
         if dq is None:
             grads.reverse()
-        return grads[0], grads[1], None, None, None, None
+        return grads[0], grads[1], None, None, None, None, None
 
 
 def _rows_ok(t):
+    if t.data_ptr() % 16 != 0:
+        return False
     unit = 16 // t.element_size()
-    return (t.stride(-1) == 1 and t.stride(-2) >= t.shape[-1] and all(s % unit == 0 for s in t.stride()[:-1])
-            and t.data_ptr() % 16 == 0)
+    return t.is_contiguous() or (t.stride(-1) == 1 and t.stride(-2) >= t.shape[-1]
+                                 and all(s % unit == 0 for s in t.stride()[:-1]))
 
 
 @dataclass
@@ -582,20 +581,20 @@ class Cache8:
 
     def _args(self, d, device):
         """Batch, heads, capacity and strides, checked."""
-        k, v = self.k, self.v
-        if k.dim() != 4 or k.element_size() != 1 or v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+        k, v, k_scale, v_scale = self.k, self.v, self.k_scale, self.v_scale
+        shape, st = k.shape, k.stride()
+        if len(shape) != 4 or k.element_size() != 1 or v.shape != shape or v.stride() != st or v.dtype != k.dtype:
             raise ValueError("the cache's k and v must be 8-bit [batch, kv_heads, capacity, d] tensors of one layout")
-        if k.shape[3] != d or k.stride(3) != 1:
+        if shape[3] != d or st[3] != 1:
             raise ValueError("the cache must have the d of the tensors, contiguous")
-        b, h, capacity, _ = k.shape
+        b, h, capacity, _ = shape
         scales = (b, h, -(-capacity // self.block))
-        for t in (self.k_scale, self.v_scale):
+        for t in (k_scale, v_scale):
             if t.dtype != torch.float32 or t.shape != scales or not t.is_contiguous():
                 raise ValueError(f"the scales must be contiguous float32 tensors of shape {scales}")
-        for t in (k, v, self.k_scale, self.v_scale):
-            if t.device != device:
-                raise ValueError("the cache must be on the device of the other tensors")
-        return b, h, capacity, _row_strides(k)
+        if k.device != device or v.device != device or k_scale.device != device or v_scale.device != device:
+            raise ValueError("the cache must be on the device of the other tensors")
+        return b, h, capacity, _row_strides(shape, st)
 
 
 def build_cache8(batch, kv_heads, capacity, d, block=64, device="cuda"):
@@ -609,50 +608,73 @@ def build_cache8(batch, kv_heads, capacity, d, block=64, device="cuda"):
 def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
     """Write new keys and values [b, kv_heads, n_new, d] (or [b, kv_heads, d]: one token) into the cache, the first
     counts[b] of sequence b at positions start[b], ... (int32 [b] on the device; None: 0, and all of them)."""
-    if k.dim() == 3:
-        k, v = k.unsqueeze(2), v.unsqueeze(2)
-    _strides(k, v)
-    b, h, n, d = k.shape
-    cb, ch, capacity, cache_strides = cache._args(d, k.device)
-    if (cb, ch) != (b, h):
+    shape, st, device, dtype = k.shape, k.stride(), k.device, k.dtype
+    if len(shape) not in (3, 4) or v.shape != shape or v.stride() != st or v.dtype != dtype or v.device != device:
+        raise ValueError("k and v must be [batch, kv_heads, n_new, d] (or [batch, kv_heads, d]) of one layout, type and GPU")
+    if device.type != "cuda" or dtype not in _DTYPE_CODES or st[-1] != 1:
+        raise ValueError("k and v must be bfloat16 or float32 on the GPU, d contiguous")
+    b, h, d = shape[0], shape[1], shape[-1]
+    cb, ch, capacity, cache_strides = cache._args(d, device)
+    if cb != b or ch != h:
         raise ValueError("k and v must have the cache's batch and heads")
-    for name, t in (("start", start), ("counts", counts)):
-        if t is not None:
-            _check_ints(name, t, (b,), k.device)
-    with _here(k.device, stream):
-        sparse_attn_cache8_store(b, h, n, d, _dtype_code(k), k, v, _row_strides(k), start, counts, capacity, cache.block,
-                                 cache.k, cache.v, cache_strides, cache.k_scale, cache.v_scale, stream)
+    if start is not None:
+        _check_ints("start", start, b, device)
+    if counts is not None:
+        _check_ints("counts", counts, b, device)
+    with _here(device, stream):
+        st = lib().sparse_attn_cache8_store(
+            b, h, shape[2] if len(shape) == 4 else 1, d, _DTYPE_CODES[dtype], k.data_ptr(), v.data_ptr(),
+            _row_strides(shape, st), None if start is None else start.data_ptr(),
+            None if counts is None else counts.data_ptr(), capacity, cache.block, cache.k.data_ptr(), cache.v.data_ptr(),
+            cache_strides, cache.k_scale.data_ptr(), cache.v_scale.data_ptr(), _stream(stream, device))
+    _check("sparse_attn_cache8_store", st)
 
 
 def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode, max_pos=None, softmax_scale=None,
             out=None, lse=None, workspace=None, stream=None):
-    """Output of one query a sequence (q: [b, h, d], at positions[b], int32 on the device; negative: no query) over the
-    8-bit cache.  ``max_pos``: an upper bound of the positions (default: the cache's last)."""
-    if q.dim() != 3 or q.stride(2) != 1 or q.device.type != "cuda":
-        raise ValueError("q must be [batch, heads, d] on the GPU, d contiguous")
-    b, h, d = q.shape
-    cb, kv_heads, capacity, cache_strides = cache._args(d, q.device)
+    """Output of one query a sequence (q: [b, h, d], at positions[b], int32 on the device) over the 8-bit cache, and its
+    log-sum-exp.  A negative position is a sequence without a query (o = 0, lse = -inf).  ``max_pos``: an upper bound of
+    the positions (default: the cache's last); above it o and lse are NaN."""
+    shape, st, device, dtype = q.shape, q.stride(), q.device, q.dtype
+    if len(shape) != 3 or st[2] != 1 or device.type != "cuda" or dtype not in _DTYPE_CODES:
+        raise ValueError("q must be [batch, heads, d] in bfloat16 or float32 on the GPU, d contiguous")
+    b, h, d = shape
+    cb, kv_heads, capacity, cache_strides = cache._args(d, device)
     if cb != b or h % kv_heads != 0:
         raise ValueError("q must have the cache's batch and a multiple of its heads")
-    _check_ints("positions", positions, (b,), q.device)
+    _check_ints("positions", positions, b, device)
     max_pos = capacity - 1 if max_pos is None else max_pos
-    dtype = _dtype_code(q)
-    need = sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, dtype)
-    with _here(q.device, stream):
-        o = torch.empty_like(q) if out is None else out
-        if o.shape != q.shape or o.stride() != q.stride() or o.dtype != q.dtype or o.device != q.device:
-            raise ValueError("out must match q in shape, strides, type and device")
-        lse = torch.empty((b, h), dtype=torch.float32, device=q.device) if lse is None else lse
-        if lse.shape != (b, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device:
+    code = _DTYPE_CODES[dtype]
+    with _here(device, stream):
+        if out is None:
+            o = torch.empty_like(q)
+            o_st = o.stride()
+        else:
+            o, o_st = out, out.stride()
+            if o.shape != shape or o.dtype != dtype or o.device != device or o_st[2] != 1:
+                raise ValueError("out must match q in shape, type and device, d contiguous")
+        if lse is None:
+            lse = torch.empty((b, h), dtype=torch.float32, device=device)
+        elif lse.shape != (b, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != device:
             raise ValueError("lse must be a contiguous float32 [batch, heads] tensor on q's device")
         if workspace is None:
-            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-        elif workspace.device != q.device:
-            raise ValueError("workspace must be on q's device")
-        sparse_attn_decode8(positions, max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, dtype, q,
-                            _longs((q.stride(0) if b > 1 else 0, q.stride(1) if h > 1 else 0)), cache.k, cache.v, cache_strides, cache.k_scale, cache.v_scale, capacity,
-                            cache.block, _scale(softmax_scale, d), o, lse, workspace,
-                            workspace.numel() * workspace.element_size(), stream)
+            size = ctypes.c_size_t()
+            _check("sparse_attn_decode8_workspace_size", lib().sparse_attn_decode8_workspace_size(
+                max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, code, ctypes.byref(size)))
+            need = size.value
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            need = workspace.numel() * workspace.element_size()
+            if workspace.device != device:
+                raise ValueError("workspace must be on q's device")
+        status = lib().sparse_attn_decode8(
+            positions.data_ptr(), max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, code, q.data_ptr(),
+            _I64x2(st[0] if b > 1 else 0, st[1] if h > 1 else 0), cache.k.data_ptr(), cache.v.data_ptr(), cache_strides,
+            cache.k_scale.data_ptr(), cache.v_scale.data_ptr(), capacity, cache.block,
+            1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale, o.data_ptr(),
+            _I64x2(o_st[0] if b > 1 else 0, o_st[1] if h > 1 else 0), lse.data_ptr(), workspace.data_ptr(), need,
+            _stream(stream, device))
+    _check("sparse_attn_decode8", status)
     return o, lse
 
 

@@ -149,12 +149,17 @@ def test_layouts_outputs_and_workspace():
     apart.v.copy_(cache.v.view(torch.uint8))
     wide = torch.zeros(2, 6, 3 * d, dtype=BF, device=dev)
     wide[..., d:2 * d] = q
-    out = torch.full((2, 6, 3 * d), 5.0, dtype=BF, device=dev)
+    out = torch.full((2, 6, 4 * d), 5.0, dtype=BF, device=dev)  # other strides than q's
     lse = torch.empty(2, 6, device=dev)
     need = sa.sparse_attn_decode8_workspace_size(299, l, c, F, MG, 2, 6, 3, d, sa.SA_BF16)
     ws = torch.full((need + 64,), 255, dtype=torch.uint8, device=dev)
     sa.decode8(wide[..., d:2 * d], apart, positions, l, c, F, MG, out=out[..., d:2 * d], lse=lse, workspace=ws[:max(need, 16)])
     assert torch.equal(out[..., d:2 * d], want[0]) and torch.equal(lse, want[1])
+    same = q[:1].expand(2, 6, d)  # one query for both sequences, a cache that both share: rows of each are read in place
+    shared = sa.Cache8(cache.k[:1].expand_as(cache.k), cache.v[:1].expand_as(cache.v), *(
+        t[:1].expand_as(t).contiguous() for t in (cache.k_scale, cache.v_scale)), 16)
+    got = sa.decode8(same, shared, torch.tensor([at[0]] * 2, dtype=torch.int32, device=dev), l, c, F, MG)
+    assert torch.equal(got[0], want[0][:1].expand_as(got[0])) and torch.equal(got[1], want[1][:1].expand_as(got[1]))
     assert torch.all(out[..., :d] == 5) and torch.all(out[..., 2 * d:] == 5) and torch.all(ws[max(need, 16):] == 255)
 
 

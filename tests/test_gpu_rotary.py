@@ -141,5 +141,10 @@ def test_gradients_against_formula_and_differences(halves):
     assert torch.equal(dk_alone, dk)
     (dq_alone,) = torch.autograd.grad(yq, (q,), w[0], retain_graph=True)
     assert torch.equal(dq_alone, dq)
-    (ones,) = torch.autograd.grad(yq.sum(), (q,))
+    (ones,) = torch.autograd.grad(yq.sum(), (q,), retain_graph=True)
     check(ones, torch.ones_like(q), turns, dims, halves, inverse=True)
+    # the gradient is linear in w: its own gradient is the rotation
+    leaf = w[0].clone().requires_grad_()
+    (dq,) = torch.autograd.grad(yq, (q,), leaf, create_graph=True)
+    (again,) = torch.autograd.grad(dq, (leaf,), q.detach())
+    assert torch.equal(again, yq)

@@ -45,6 +45,7 @@ ROTARY = dict(batch=2, n=8, qh=4, kh=2, d=64, dtype=sa.SA_BF16, q=FAKE, qs=longs
     (dict(d=48), UNS), (dict(dtype=2), INV), (dict(q=None), INV), (dict(q=FAKE + 8), INV), (dict(qo=FAKE + 2), INV),
     (dict(qs=longs(2048, 512, 32)), INV), (dict(qs=longs(2048, 516, 64)), INV), (dict(qos=longs(-8, 512, 64)), INV),
     (dict(qs=longs(4096, 512, 64)), INV),  # its own output with other strides
+    (dict(qos=longs(2048, 0, 64)), INV), (dict(qos=longs(0, 512, 64)), INV),  # rows that two heads would write
     (dict(k=None), INV), (dict(ko=None), INV), (dict(kos=None), INV), (dict(ks=longs(1024, 512, 68)), INV),
     (dict(pos=None), INV), (dict(pos=FAKE + 2), INV), (dict(ps=None), INV), (dict(ps=longs(-1, 2)), INV),
     (dict(axes=0), INV), (dict(axes=5), INV), (dict(dims=ints(31, 32)), INV), (dict(dims=ints(0, 32)), INV),
@@ -67,6 +68,7 @@ STORE = dict(batch=2, kvh=4, n=8, d=64, dtype=sa.SA_BF16, k=FAKE, v=FAKE, ks=lon
     (dict(counts=FAKE + 2), INV), (dict(capacity=0), INV), (dict(capacity=2 ** 31), INV), (dict(block=48), INV),
     (dict(block=256), INV), (dict(kc=None), INV), (dict(vc=FAKE + 8), INV), (dict(cs=None), INV),
     (dict(cs=longs(51200, 12800, 48)), INV), (dict(cs=longs(51200, 12808, 128)), INV), (dict(ksc=None), INV),
+    (dict(cs=longs(0, 12800, 128)), INV), (dict(cs=longs(51200, 0, 128)), INV),  # rows that two would write
     (dict(vsc=FAKE + 2), INV), (dict(batch=2 ** 20, n=2 ** 20), UNS),
 ])
 def test_store_refusals(L, over, expect):
@@ -75,7 +77,7 @@ def test_store_refusals(L, over, expect):
 
 DECODE = dict(pos=FAKE, max_pos=99, l=16, c=0, pattern=sa.SA_STRIDED, mode=sa.SA_MODE_MERGED, batch=2, heads=4, kvh=2, d=64,
               dtype=sa.SA_BF16, q=FAKE, qs=longs(256, 64), kc=FAKE, vc=FAKE, cs=longs(12800, 6400, 64), ksc=FAKE, vsc=FAKE,
-              capacity=100, block=16, scale=0.125, o=FAKE, lse=FAKE, ws=FAKE, wsb=1 << 30, stream=None)
+              capacity=100, block=16, scale=0.125, o=FAKE, os=longs(256, 64), lse=FAKE, ws=FAKE, wsb=1 << 30, stream=None)
 
 
 @pytest.mark.parametrize("over,expect", [
@@ -85,7 +87,8 @@ DECODE = dict(pos=FAKE, max_pos=99, l=16, c=0, pattern=sa.SA_STRIDED, mode=sa.SA
     (dict(d=16), UNS), (dict(dtype=-1), INV), (dict(q=FAKE + 4), INV), (dict(qs=longs(256, 60)), INV), (dict(qs=None), INV),
     (dict(kc=None), INV), (dict(vc=FAKE + 4), INV), (dict(cs=longs(12800, 6400, 32)), INV), (dict(ksc=None), INV),
     (dict(capacity=0), INV), (dict(block=8), INV), (dict(scale=0.0), INV), (dict(scale=float("nan")), INV),
-    (dict(o=None), INV), (dict(lse=None), INV), (dict(lse=FAKE + 2), INV), (dict(ws=None), INV), (dict(ws=FAKE + 8), INV),
+    (dict(o=None), INV), (dict(os=None), INV), (dict(os=longs(0, 64)), INV), (dict(os=longs(256, 56)), INV),
+    (dict(os=longs(256, 68)), INV), (dict(lse=None), INV), (dict(lse=FAKE + 2), INV), (dict(ws=None), INV), (dict(ws=FAKE + 8), INV),
     (dict(wsb=0), SMALL), (dict(batch=2 ** 20, heads=8), UNS),
 ])
 def test_decode8_refusals(L, over, expect):
