@@ -150,11 +150,14 @@ __device__ inline void wave_order() {
 }
 
 // Lane (g, r) = 16 g + r.  Key u of a chunk: row 4 g' + i of tile j for u = 8 g' + 4 j + i.
+// (bf16 of d = 32 is one register over what six waves a SIMD may have: 256 units, 8,416 keys 33.7
+// -> 31.9 us held to them.)
 template <int D, typename T, int NWV, bool DIRECT>
-__global__ void __launch_bounds__(NWV * 64)
+__global__ void __launch_bounds__(NWV * 64, D == 32 && sizeof(T) == 2 ? 6 : 1)
 decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__ part, T* __restrict__ o,
                      float* __restrict__ lse) {
     constexpr int QP = sizeof(T) == 2 ? 1 : 3;   // pieces of a query
+    constexpr int PP = sizeof(T) == 2 ? 2 : 3;   // pieces of a weight
     constexpr int FK = D / 32, TV = D / 16;      // 32-deep products of K; 16-element tiles of V
     constexpr int PR = D / 8;                    // 16-byte pieces of a key's rows
     union Lds {
@@ -284,20 +287,27 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
             s[0][i] *= v0[i];
             s[1][i] *= v1[i];
         }
-        // weights in bf16: a bf16 result is rounded no finer than each of them; an fp32 result takes a second
-        // piece for the remainder (2^-17 of a weight)
-        bf16x8 hi, lo;
-        if constexpr (QP == 1)
-            hi = pack_bf16x8(s[0], s[1]);
-        else
-            split_bf16x8(s[0], s[1], hi, lo);
+        // the weights as bf16 pieces that sum to them: two (2^-16 of a weight) for bf16 results, three (all 24 bits)
+        // for fp32.  One piece would round a weight no finer than the result is: a set of a few keys
+        // then came out a third further from the exact result, for 2% less time (32 sequences: 46.2 us, two
+        // pieces 46.9, three 47.8); two pieces for fp32 were 2^-20 off, ten times its own rounding.
+        bf16x8 pf[PP];
+#pragma unroll
+        for (int k = 0; k < PP; ++k) {
+            pf[k] = pack_bf16x8(s[0], s[1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[0][i] -= (float)pf[k][i];
+                s[1][i] -= (float)pf[k][4 + i];
+            }
+        }
 #pragma unroll
         for (int t = 0; t < TV; ++t) {
             // lane i of a row of 16 gets element 16 t + i of keys 8 g .. 8 g + 7
             const u32x2 v8 = ld_tr8(mine.rows + (8 * g + r / 2) * WaveLds<D>::kPitch + D + 16 * t + 8 * (r % 2));
             const bf16x8 vf = scaled8(v8[0], v8[1], 1.f);
-            acc[t] = mfma_16x16x32(vf, hi, acc[t]);
-            if constexpr (QP != 1) acc[t] = mfma_16x16x32(vf, lo, acc[t]);
+#pragma unroll
+            for (int k = PP - 1; k >= 0; --k) acc[t] = mfma_16x16x32(vf, pf[k], acc[t]);
         }
         wave_order();  // read before the next chunk is written
     };
@@ -442,11 +452,11 @@ hipError_t launch(const Decode8Args& a, int batch, const void* q, void* o, float
 // Ranges per unit, for the largest set that a position up to max_pos can have.
 //   One range up to 256 keys, two chunks a wave: there is nothing to join (8 heads of 64, 206 keys: one
 //   launch 4.8 us, two ranges 6.7).
-//   Else at least 128 keys a range, one chunk a wave: the fewer serial steps the better, while
-//   there are few workgroups (8 cache heads of 64, 736 keys: 256 keys a range 7.6 us, 128
+//   Else 128 keys a range, one chunk a wave: the fewer serial steps the better, while there are few
+//   workgroups (8 cache heads of 64, 736 keys: 256 keys a range 7.6 us, 128
 //   7.2; d = 128 fp32, 2,272 keys 11.3 | 9.4).
-//   From 512 workgroups on (1,024 for d <= 64, whose waves have less on their way) longer
-//   ranges instead, as every range costs the join (8 sequences, 4 cache heads, d = 128, 8,416
+//   From 512 workgroups on (1,024 for d <= 64, whose waves have less on their way; a quarter more before
+//   a wave takes a second chunk) just so many, with longer ranges, as every range costs the join (8 sequences, 4 cache heads, d = 128, 8,416
 //   keys: 2,112 workgroups 25.2, 1,024 20.4, 512 18.9), and at most 128 ranges a unit (one unit,
 //   65,760 keys: 512 ranges 15.1 us, 128 11.6).
 //   Where that leaves more than 2,048 keys a range, ranges of about 1,024 (512 for d <= 64): walks of
@@ -468,7 +478,8 @@ int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, in
         }
     }
     if (count <= 256) return 1;
-    const int64_t few = max64(min64(min64((count + 127) / 128, (d == 128 ? 512 : 1024) / units), 128), 1);
+    const int64_t finest = (count + 127) / 128, target = d == 128 ? 512 : 1024;
+    const int64_t few = max64(min64(units * finest * 4 <= target * 5 ? finest : target / units, 128), 1);
     if (count <= 2048 * few) return (int)few;
     int64_t many = min64(min64(count / (d == 128 ? 1024 : 512), 4096 / rows), 512);
     const int64_t rounds = units * many / 1024;

@@ -654,7 +654,7 @@ def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode
             if o.shape != shape or o.dtype != dtype or o.device != device or o_st[2] != 1:
                 raise ValueError("out must match q in shape, type and device, d contiguous")
         if lse is None:
-            lse = torch.empty((b, h), dtype=torch.float32, device=device)
+            lse = q.new_empty((b, h), dtype=torch.float32)
         elif lse.shape != (b, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != device:
             raise ValueError("lse must be a contiguous float32 [batch, heads] tensor on q's device")
         if workspace is None:
@@ -662,7 +662,7 @@ def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode
             _check("sparse_attn_decode8_workspace_size", lib().sparse_attn_decode8_workspace_size(
                 max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, code, ctypes.byref(size)))
             need = size.value
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            workspace = q.new_empty(need, dtype=torch.uint8)
         else:
             need = workspace.numel() * workspace.element_size()
             if workspace.device != device:

@@ -110,7 +110,7 @@ def test_decode8_matches_64_bits(pattern, mode, capacity, l, c, d, dtype, heads,
 @pytest.mark.parametrize("batch,heads,kv_heads,d,dtype,keys", [
     (1, 1, 1, 64, BF, 1), (1, 2, 2, 128, FP, 31), (1, 1, 1, 32, BF, 255), (2, 192, 192, 32, FP, 256), (1, 385, 385, 32, BF, 256),
     (1, 192, 192, 32, BF, 257), (1, 1, 1, 64, BF, 5000), (2, 2, 2, 128, BF, 2100), (1, 64, 4, 64, FP, 2100),
-    (3, 300, 3, 32, BF, 300), (64, 8, 8, 32, BF, 2100),
+    (3, 300, 3, 32, BF, 300), (64, 8, 8, 32, BF, 2100), (64, 16, 16, 32, BF, 2100), (5, 24, 24, 128, FP, 700),
 ])
 def test_launch_rules(batch, heads, kv_heads, d, dtype, keys):
     dev = device()
