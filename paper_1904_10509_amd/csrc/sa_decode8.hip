@@ -98,33 +98,6 @@ __device__ inline void query_pieces(const float* p, bf16x8* x) {
     }
 }
 
-// S_position as an index space (DecodeSet) in 32 bits: key t is lo + t within A1, and
-// with u = t - near behind it base + u + floor(u / c) * step: the summary columns (step =
-// l - c), or one multiple of l after the other (c = 1, step = -l - 1).
-struct KeySet {
-    uint32_t near, count;
-    int32_t lo, base, step;
-    bool alone;  // c = 1: floor(u / c) = u, which the division's 32 upper bits do not give
-    uint32_t m, shift;
-    __device__ KeySet(const DecodeSet& s) {
-        const bool a2 = s.part == PART_A2;
-        near = a2 ? 0 : (uint32_t)s.n1;
-        count = (uint32_t)s.count;
-        lo = s.a1_lo;
-        const bool strided = s.pattern == STRIDED;
-        base = strided ? (a2 ? s.pos : s.pos - 2 * s.l) : s.w;
-        step = strided ? -s.l - 1 : s.l - s.c;
-        alone = strided || s.c == 1;
-        m = s.dc.m;
-        shift = alone ? 0u : (uint32_t)(s.dc.shift - 32);
-    }
-    __device__ int32_t at(uint32_t t) const {
-        const int32_t u = (int32_t)(t - near);
-        const int32_t q = alone ? u : (int32_t)(__umulhi((uint32_t)u, m) >> shift);
-        return t < near ? lo + (int32_t)t : base + u + q * step;
-    }
-};
-
 // What a wave has in LDS: a chunk's rows (K, then V, of a key), their scales and their
 // places in the cache.  The pitch of 16 bytes more than a row spreads the 16 rows that a
 // read of K takes over the banks.

@@ -217,8 +217,8 @@ struct DecodeSet {
         } else {
             a1_lo = lblk * l;
             n1 = (int64_t)pos - a1_lo + 1;
-            const int32_t first_sum = a1_lo + w;  // first summary column of pos's l-block
-            const int32_t own = pos >= first_sum ? (pos - first_sum + 1 < c ? pos - first_sum + 1 : c) : 0;
+            const int32_t past = pos - a1_lo - w;  // columns from the first summary one of pos's l-block to pos
+            const int32_t own = past >= 0 ? (past < c ? past + 1 : c) : 0;
             if (part == PART_A1) count = n1;
             else if (part == PART_A2) count = (int64_t)lblk * c + own;
             else count = n1 + (int64_t)lblk * c;
@@ -237,6 +237,32 @@ struct DecodeSet {
         if (part == PART_A2) return summary((int32_t)t);
         if (t < n1) return a1_lo + (int32_t)t;
         return summary((int32_t)(t - n1));
+    }
+};
+
+// The same index space in 32 bits and without a branch on the pattern: key t is lo + t within A1, and
+// with u = t - near behind it base + u + floor(u / c) * step: the summary columns (step =
+// l - c), or one multiple of l after the other (c = 1, step = -l - 1).
+struct KeySet {
+    uint32_t near, count;
+    uint32_t lo, base, step;  // modulo 2^32: base and step can be negative, positions are not
+    bool alone;  // c = 1: floor(u / c) = u, which the division's 32 upper bits do not give
+    uint32_t m, shift;
+    __host__ __device__ explicit KeySet(const DecodeSet& s) {
+        const bool a2 = s.part == PART_A2;
+        near = a2 ? 0 : (uint32_t)s.n1;
+        count = (uint32_t)s.count;
+        lo = (uint32_t)s.a1_lo;
+        const bool strided = s.pattern == STRIDED;
+        base = strided ? (uint32_t)s.pos - (a2 ? 0u : 2u * (uint32_t)s.l) : (uint32_t)s.w;
+        step = strided ? ~(uint32_t)s.l : (uint32_t)(s.l - s.c);  // ~l = -l - 1
+        alone = strided || s.c == 1;
+        m = s.dc.m;
+        shift = alone ? 0u : (uint32_t)(s.dc.shift - 32);
+    }
+    __host__ __device__ int32_t at(uint32_t t) const {
+        const uint32_t u = t - near, q = alone ? u : (uint32_t)((uint64_t)u * m >> 32) >> shift;
+        return (int32_t)(t < near ? lo + t : base + u + q * step);
     }
 };
 

@@ -158,12 +158,13 @@ def test_reference_codes_match_torch():
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
-def test_scale_exponent_on_the_host(tmp_path):
-    """The library's exponent (csrc/sa_e4m3.h) against the definition, around every border."""
-    exe = tmp_path / "check_scale"
+@pytest.mark.parametrize("program", ["check_scale", "check_key_set"])
+def test_host_arithmetic(tmp_path, program):
+    """The scales' exponents (csrc/sa_e4m3.h) and the step's index space (KeySet, csrc/sa_pattern.h) against their
+    definitions, around every border."""
+    exe = tmp_path / program
     subprocess.run([HIPCC, "-O2", "-std=c++17", *SAN, "-I", os.path.join(ROOT, "paper_1904_10509_amd", "csrc"),
-                    os.path.join(ROOT, "tests", "host", "check_scale.cpp"), "-o", str(exe)], check=True,
-                   capture_output=True)
+                    os.path.join(ROOT, "tests", "host", program + ".cpp"), "-o", str(exe)], check=True, capture_output=True)
     out = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300,
                          env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
     assert out.returncode == 0 and out.stdout.startswith("ok"), out.stdout + out.stderr
