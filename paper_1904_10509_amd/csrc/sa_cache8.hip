@@ -20,6 +20,12 @@ namespace sa {
 
 namespace {
 
+// Up to here K and V of a block go to workgroups of their own, as a call of few blocks is bound by the
+// latency of one (one token, 32 sequences, 8 heads: 3.6 -> 3.2 us; 1,501 tokens, 2 x 4 heads of 128, fp32, 104 blocks:
+// 6.9 -> 5.1).  From there on one workgroup writes both, so that where they interleave a line's two halves
+// meet in one L2 (520 blocks: the same; 776 of d = 128 15.8 -> 15.1; 49,216 of 16 tokens 69.0 -> 56.5).
+constexpr int64_t kFewGroups = 512;
+
 struct StoreArgs {
     Cache8 c;
     int32_t kv_heads, n_new, reach;  // reach: blocks that the new tokens of a sequence can lie in
@@ -89,13 +95,13 @@ __device__ inline uint32_t group_max(uint32_t x, uint32_t* s) {
     return x;
 }
 
-// NT threads, CH pieces each: NT * CH = the pieces of a block.
-template <typename T, int NT, int CH>
+// NT threads, CH pieces each: NT * CH = the pieces of a block.  TENSORS: 2, or 1 with blockIdx.y for which.
+template <typename T, int NT, int CH, int TENSORS>
 __global__ void __launch_bounds__(NT)
 store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
     constexpr int E = Piece<T>::kElements;
     typedef typename Piece<T>::Codes Codes;
-    __shared__ uint32_t s_max[4][NT / 64], s_old[2];
+    __shared__ uint32_t s_max[2 * TENSORS][NT / 64], s_old[TENSORS];
     const int tid = threadIdx.x;
     const uint32_t id = blockIdx.x, row = id / (uint32_t)a.reach;
     const int r = (int)(id - row * (uint32_t)a.reach);
@@ -111,28 +117,30 @@ store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
     const int lo = (int)max64(start - first, 0), hi = (int)min64(end - first, (int64_t)1 << a.c.block_shift);
     const int64_t from = b * a.xb + h * a.xh + (first - start) * a.xs;  // of the block's first row (before k where lo > 0)
     const int mask = (1 << a.row_shift) - 1;
-    Piece<T> x[2][CH];
+    Piece<T> x[TENSORS][CH];
+    auto is_v = [](int t) { return TENSORS == 1 ? blockIdx.y == 1 : t == 1; };
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int piece = i * NT + tid, at = piece >> a.row_shift;
         const int64_t off = from + at * a.xs + (piece & mask) * E;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            if (at >= lo && at < hi) x[t][i].load((t ? v : k) + off);
+        for (int t = 0; t < TENSORS; ++t) {
+            if (at >= lo && at < hi) x[t][i].load((is_v(t) ? v : k) + off);
             else x[t][i].u = u32x4{0, 0, 0, 0};
         }
     }
-    float* scale[2] = {a.c.ks + (int64_t)row * a.c.blocks + blk, a.c.vs + (int64_t)row * a.c.blocks + blk};
-    if (tid < 2) s_old[tid] = lo > 0 ? __float_as_uint(*scale[tid]) : 0u;
-    uint32_t top[2] = {0, 0};
+    const int64_t at_scale = (int64_t)row * a.c.blocks + blk;
+    if (tid < TENSORS) s_old[tid] = lo > 0 ? __float_as_uint((is_v(tid) ? a.c.vs : a.c.ks)[at_scale]) : 0u;
+    uint32_t top[TENSORS];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < TENSORS; ++t) {
+        top[t] = 0;
 #pragma unroll
         for (int i = 0; i < CH; ++i) grow(top[t], x[t][i]);
         top[t] = group_max<NT>(largest(top[t], k), s_max[t]);
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < TENSORS; ++t) {
         const bool fine = finite_bits(top[t]);
         if (!fine) {  // (the same for the whole workgroup) an infinity or a NaN: the largest of the others
             top[t] = 0;
@@ -143,7 +151,7 @@ store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
                     const uint32_t m = x[t][i].bits(e) & 0x7fffffffu;
                     if (finite_bits(m)) top[t] = max(top[t], m);
                 }
-            top[t] = group_max<NT>(top[t], s_max[2 + t]);
+            top[t] = group_max<NT>(top[t], s_max[TENSORS + t]);
         }
         int e_new = scale_exponent(top[t]);
         int growth = 0;  // of the scale of earlier tokens
@@ -153,7 +161,7 @@ store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
             growth = e_new - e_old;
         }
         const float unit = __uint_as_float(power_bits(e_new));
-        uint8_t* codes = (t ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh + first * a.c.ss;
+        uint8_t* codes = (is_v(t) ? a.c.v : a.c.k) + b * a.c.sb + h * a.c.sh + first * a.c.ss;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int piece = i * NT + tid, at = piece >> a.row_shift;
@@ -170,13 +178,17 @@ store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
                 *dst = rescaled(*dst, __uint_as_float(power_bits(growth < 126 ? -growth : -126)));
             }
         }
-        if (tid == 0) *scale[t] = unit;
+        if (tid == 0) (is_v(t) ? a.c.vs : a.c.ks)[at_scale] = unit;
     }
 }
 
 template <typename T, int NT, int CH>
 hipError_t launch(const StoreArgs& a, int64_t groups, const void* k, const void* v, hipStream_t stream) {
-    hipLaunchKernelGGL((store_kernel<T, NT, CH>), dim3((unsigned)groups), dim3(NT), 0, stream, a, (const T*)k, (const T*)v);
+    const T *kt = (const T*)k, *vt = (const T*)v;
+    if (groups < kFewGroups)
+        hipLaunchKernelGGL((store_kernel<T, NT, CH, 1>), dim3((unsigned)groups, 2), dim3(NT), 0, stream, a, kt, vt);
+    else
+        hipLaunchKernelGGL((store_kernel<T, NT, CH, 2>), dim3((unsigned)groups), dim3(NT), 0, stream, a, kt, vt);
     return hipGetLastError();
 }
 

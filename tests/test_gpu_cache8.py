@@ -76,6 +76,17 @@ def test_store_matches_definition(batch, heads, capacity, d, block, dtype, n, st
     store_and_check(cache, k, v, start, counts)
 
 
+# 512 blocks and more: K and V by one workgroup, in every shape of it
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,block", [(32, 16), (64, 16), (64, 32), (64, 64), (128, 64), (128, 128)])
+def test_many_blocks(d, block, dtype):
+    batch, heads, n = 16, 16, block + 2  # up to three blocks each
+    cache = fresh(batch, heads, 3 * block, d, block, seed=d)
+    k, v = make((batch, heads, n, d), dtype, d + block), make((batch, heads, n, d), dtype, d + block + 1)
+    k[3, 2, 1, 4], v[5, 5, 0, 0] = float("nan"), float("inf")
+    store_and_check(cache, k, v, [b * (block // 16) for b in range(batch)], [n - b % 3 for b in range(batch)])
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_token_by_token(dtype):
     """Tokens that grow and shrink, one at a time over two blocks: scales only grow inside a block, old codes follow."""
