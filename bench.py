@@ -251,7 +251,8 @@ DECODE = {
 def decode_bench(args):
     """Time per decoding step (sparse_attn_decode at positions n - steps .. n - 1,
     one per step, as in generation) and the bandwidth of the K / V rows it
-    reads (|S_pos| rows of K and of V per (sequence, head)) against HBM."""
+    reads (|S_pos| rows of K and of V per (sequence, head)) against HBM; the same
+    over an 8-bit cache of these keys and values (sparse_attn_decode8)."""
     import torch
 
     from paper_1904_10509_amd import sparse_attn as sa
@@ -279,16 +280,32 @@ def decode_bench(args):
             sa.decode(qs[s], kc, vc, positions[s], c["l"], c["c"], c["pattern"], sa.SA_MODE_MERGED,
                       out=o, lse=lse, workspace=ws)
 
-        for s in range(args.warmup):
-            step(s)
-        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        torch.cuda.synchronize()
-        e0.record()
-        for s in range(args.warmup, total):
-            step(s)
-        e1.record()
-        torch.cuda.synchronize()
-        us = e0.elapsed_time(e1) * 1e3 / args.steps
+        def timed(step):
+            for s in range(args.warmup):
+                step(s)
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            e0.record()
+            for s in range(args.warmup, total):
+                step(s)
+            e1.record()
+            torch.cuda.synchronize()
+            return e0.elapsed_time(e1) * 1e3 / args.steps
+
+        us = timed(step)
+        # the same steps over the same keys and values in 8 bits
+        cache = sa.build_cache8(c["batch"], c["heads"], c["n"], c["d"], device=dev)
+        sa.store8(cache, kc, vc)
+        places = torch.tensor(positions, dtype=torch.int32, device=dev)[:, None].repeat(1, c["batch"])
+        ws8 = torch.empty(sa.sparse_attn_decode8_workspace_size(c["n"] - 1, c["l"], c["c"], c["pattern"],
+                                                                sa.SA_MODE_MERGED, c["batch"], c["heads"], c["heads"],
+                                                                c["d"], sa.SA_BF16), dtype=torch.uint8, device=dev)
+
+        def step8(s):
+            sa.decode8(qs[s], cache, places[s], c["l"], c["c"], c["pattern"], sa.SA_MODE_MERGED, out=o, lse=lse,
+                       workspace=ws8)
+
+        us8 = timed(step8)
         # |S_pos| of the merged sets (closed forms of Sec. 4.3, the same for every
         # summary subblock), averaged over the timed positions
         rows = 0
@@ -305,7 +322,12 @@ def decode_bench(args):
                                "tokens_per_s": c["batch"] / (us * 1e-6),
                                "roofline": {"bound": "hbm", "achieved": gbs, "peak": HBM_PEAK_GBS, "unit": "GB/s",
                                             "frac": gbs / HBM_PEAK_GBS}}
-        del kc, vc
+        gbs8 = 0.5 * kv_bytes / (us8 * 1e-6) / 1e9  # a byte an element
+        out["shapes"][name]["cache8"] = {"us_per_step": us8, "kv_bytes_per_step": 0.5 * kv_bytes,
+                                         "tokens_per_s": c["batch"] / (us8 * 1e-6),
+                                         "roofline": {"bound": "hbm", "achieved": gbs8, "peak": HBM_PEAK_GBS,
+                                                      "unit": "GB/s", "frac": gbs8 / HBM_PEAK_GBS}}
+        del kc, vc, cache
         torch.cuda.empty_cache()
     print(json.dumps(out), flush=True)
 
