@@ -326,7 +326,7 @@ int sparse_attn_decode(int64_t pos, int32_t stride_l, int32_t summary_c, int32_t
  *                  any int32, negative ones included
  *   n              1 <= n < 2^31 (n = 1: the new token of every sequence)
  *   n_axes         1 .. 4
- * Angles are exact to 2^-31 turns at every place; products in fp32, one rounding at
+ * Angles are exact to 2^-29 turns at every place; products in fp32, one rounding at
  * the end.  Every base address 16-byte aligned and every stride of q, k and the
  * outputs a multiple of 16 bytes, token strides >= d_head, rows of an output apart; positions 4-byte
  * aligned, strides >= 0.  d_head in {32, 64, 128}; batch * n < 2^33 and at most
@@ -367,7 +367,9 @@ int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_head
  * ties to even.  Where start[b] lies inside a block, its earlier tokens stay:
  * the new scale is at least the old one, and where it grows, their codes become
  * the nearest e4m3 to code * (old scale / new scale), which is exact but for
- * codes that turn subnormal.  Positions of the block behind the new tokens keep
+ * codes that turn subnormal.  (A scale of 0 is a block that holds nothing yet: fill
+ * the scales of a new cache with zeros where a first store can begin inside a
+ * block.)  Positions of the block behind the new tokens keep
  * their bytes but not their meaning (the scale is the block's).  A NaN or an
  * infinity is stored as NaN and has no part in the scale.  Rows of different
  * sequences and heads of the cache must not overlap.

@@ -8,9 +8,9 @@
 // pairs of one token and makes their sines and cosines once for several heads.
 //
 // The angle in turns is p f / (2 pi) modulo 1.  With F = f / (2 pi) in units of
-// 2^-64 turns, the low 64 bits of the integer product p F are that fraction, with
-// an error of p 2^-65 turns at most and no range reduction: places of millions lose
-// nothing.  Its upper 32 bits, read as signed, are the turn in [-1/2, 1/2).
+// 2^-64 turns, the low 64 bits of the integer product p F are that fraction, off by
+// p times F's own error (2^-60.3, so 2^-29 turns at the furthest place) and with no range
+// reduction: places of millions lose nothing.  Its upper 32 bits, read as signed, are the turn in [-1/2, 1/2).
 #include <math.h>
 
 #include "sa_internal.h"
@@ -200,8 +200,8 @@ hipError_t rotary_launch(const RotaryCall& c, hipStream_t stream) {
     a.tokens = c.n * c.batch;
     a.axes = c.axes;
     a.sign = c.inverse ? -1.f : 1.f;
-    // F by repeated products in extended precision (64 bits of mantissa): a few units
-    // of 2^-64 off at the last of 64 pairs.  No turn of a whole pair reaches 2^64: f <= 1.
+    // F by repeated products in extended precision (64 bits of mantissa): pair t is off by about
+    // 2 t 2^-64 f_t turns, which falls with f_t: 13 units of 2^-64 at most (base 1.5, 64 pairs).
     int pair = 0;
     int w = 8;
     for (int x = 0; x < c.axes; ++x) {

@@ -601,7 +601,7 @@ def build_cache8(batch, kv_heads, capacity, d, block=64, device="cuda"):
     """An empty 8-bit cache.  A token's key and value lie side by side: the patterns that gather single tokens read
     them in one piece."""
     kv = torch.empty((batch, kv_heads, capacity, 2, d), dtype=torch.float8_e4m3fn, device=device)
-    scales = torch.empty((2, batch, kv_heads, -(-capacity // block)), dtype=torch.float32, device=device)
+    scales = torch.zeros((2, batch, kv_heads, -(-capacity // block)), dtype=torch.float32, device=device)  # 0: nothing yet
     return Cache8(kv[..., 0, :], kv[..., 1, :], scales[0], scales[1], block)
 
 

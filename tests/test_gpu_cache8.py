@@ -99,6 +99,25 @@ def test_token_by_token(dtype):
     assert all(np.array_equal(a, b) for a, b in zip(state(cache), again))
 
 
+def test_first_store_inside_a_block():
+    """A new cache (scales of 0) whose first token lies inside a block: the scale is the new tokens' own."""
+    cache = sa.build_cache8(2, 2, 64, 32, 32, device=device())
+    cache.k.copy_(torch.full(cache.k.shape, 0x7B, dtype=torch.uint8).view(torch.float8_e4m3fn))  # what was there before
+    cache.v.copy_(torch.full(cache.v.shape, 0x7B, dtype=torch.uint8).view(torch.float8_e4m3fn))
+    x = make((2, 2, 9, 32), torch.bfloat16, 6)
+    sa.store8(cache, x.to(device()), x.to(device()), torch.tensor([5, 30], dtype=torch.int32, device=device()))
+    torch.cuda.synchronize()
+    for b, start in enumerate((5, 30)):
+        for h in range(2):
+            for blk in range(start // 32, (start + 8) // 32 + 1):
+                r0, r1 = max(start, 32 * blk), min(start + 9, 32 * blk + 32)
+                new = to64(x)[b, h, r0 - start:r1 - start]
+                e = ref.scale_exponent(np.abs(new).max())
+                for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+                    assert float(scale[b, h, blk]) == 2.0 ** e
+                    assert np.array_equal(codes[b, h, r0:r1].view(torch.uint8).cpu().numpy(), ref.e4m3_encode(new * 2.0 ** -e))
+
+
 def test_every_bf16_value():
     """All 65,536 bit patterns: each at the scale of its own row's block (the largest finite ones, subnormals, NaN and
     infinities among them), then all of e4m3's borders at scale 1."""

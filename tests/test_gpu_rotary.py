@@ -1,7 +1,7 @@
 """Rotary positions of several axes against 64 bits.
 
-Bounds, per element with its pair's |x0| + |x1| = S.  The angle is cut to 2^-32 turns, becomes a float (half a step of
-2^-25 below half a turn) and its sine and cosine are off by 2^-22 each at most: 2 pi (2^-32 + 2^-26) + 2^-22 = 3.4e-7,
+Bounds, per element with its pair's |x0| + |x1| = S.  The angle is off by 2^-29 turns, becomes a float (half a step of
+2^-25 below half a turn) and its sine and cosine are off by 2^-22 each at most: 2 pi (2^-29 + 2^-26) + 2^-22 = 3.5e-7,
 times S; two products and a sum round by 2^-24 of S each, 1.8e-7 S.  6e-7 S in fp32.  For bf16 outputs the sines and
 cosines may be off by 2^-14, which S carries into y below the rounding of y itself: 2^-14 S + 2^-8 |y|."""
 import numpy as np
