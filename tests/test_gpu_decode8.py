@@ -163,6 +163,20 @@ def test_layouts_outputs_and_workspace():
     assert torch.all(out[..., :d] == 5) and torch.all(out[..., 2 * d:] == 5) and torch.all(ws[max(need, 16):] == 255)
 
 
+def test_positions_of_any_value():
+    """The ends of int32 and the neighbours of the bound, in a batch whose other rows stay as they are."""
+    dev, d = device(), 64
+    cache, values = make_cache(6, 1, 300, d, 32, 7, [299] * 6)
+    q = torch.randn((6, 2, d), generator=torch.Generator().manual_seed(4)).to(BF).to(dev)
+    at = [299, -2 ** 31, 280, 281, 2 ** 31 - 1, 0]
+    o, lse = sa.decode8(q, cache, torch.tensor(at, dtype=torch.int32, device=dev), 30, 0, S, MG, max_pos=280)
+    torch.cuda.synchronize()
+    above = torch.tensor([p > 280 for p in at])
+    assert torch.isnan(o[above]).all() and torch.isnan(lse[above]).all()
+    keep = [i for i, p in enumerate(at) if p <= 280]
+    check(o[keep], lse[keep], q[keep], [v[keep] for v in values], [max(at[i], -1) for i in keep], 30, 0, S, MG, d ** -0.5)
+
+
 def test_offsets_past_32_bits():
     """Positions behind 2^31 and 2^32 bytes of one sequence's cache."""
     dev, d, block, capacity, l = device(), 128, 128, 20_000_000, 70_001

@@ -148,3 +148,16 @@ def test_gradients_against_formula_and_differences(halves):
     (dq,) = torch.autograd.grad(yq, (q,), leaf, create_graph=True)
     (again,) = torch.autograd.grad(dq, (leaf,), q.detach())
     assert torch.equal(again, yq)
+
+
+def test_long_sequences_by_slices():
+    """Nine million tokens of 128 in pieces of one pair each (2.3 GB a tensor, more workgroups than one grid row holds):
+    slices around the borders give the bits of calls of their own."""
+    dev, n, d, dims = device(), 9_000_000, 128, (2,)
+    x = torch.randn((1, 1, n, d), generator=torch.Generator(device=dev).manual_seed(1), device=dev, dtype=torch.bfloat16)
+    places = torch.arange(n, dtype=torch.int32, device=dev)[:, None]
+    y, _ = sa.rotary(x, None, places, dims, pairing=HALF)
+    for at in (0, 4_194_304 - 50, 8_388_608 - 50, 2 ** 30 // 128 - 50, n - 100):
+        part, _ = sa.rotary(x[:, :, at:at + 100].contiguous(), None, places[at:at + 100], dims, pairing=HALF)
+        assert torch.equal(y[:, :, at:at + 100], part), at
+    assert torch.equal(y[..., 2:], x[..., 2:])
