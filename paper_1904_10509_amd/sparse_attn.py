@@ -488,6 +488,52 @@ def grid_positions(shape, device="cuda"):
     return torch.stack([a.reshape(-1) for a in axes], dim=1)
 
 
+def _rotary_args(q, k, positions, axis_dims, base, pairing):
+    """What a call on tensors of these shapes passes in front of them and behind them, checked."""
+    shape, device, dtype = q.shape, q.device, q.dtype
+    k_shape = shape if k is None else k.shape
+    # (every attribute of a tensor is a call into torch: each is read once)
+    if len(shape) not in (3, 4) or len(k_shape) != len(shape) or k_shape[0] != shape[0] or k_shape[2:] != shape[2:]:
+        raise ValueError("q and k must be [batch, heads, n, d] (or [batch, heads, d]) of one batch, n and d")
+    if device.type != "cuda" or dtype not in _DTYPE_CODES or k is not None and (k.device != device or k.dtype != dtype):
+        raise ValueError("q and k must share type and GPU, in bfloat16 or float32")
+    single = len(shape) == 3
+    b, n, d, axes = shape[0], 1 if single else shape[2], shape[-1], len(axis_dims)
+    places, p_st = positions.shape, positions.stride()
+    shared = not single and places in ((n, axes), (1, n, axes))
+    if not shared and places != ((b, axes) if single else (b, n, axes)):
+        raise ValueError("positions must be [n, axes] or [batch, n, axes] (one token: [batch, axes])")
+    if positions.dtype != torch.int32 or positions.device != device or axes > 1 and p_st[-1] != 1:
+        raise ValueError("positions must be int32 with the axes contiguous, on the device of q and k")
+    return ((b, n, shape[1], 0 if k is None else k_shape[1], d, _DTYPE_CODES[dtype]),
+            (positions.data_ptr(), _I64x2(0, p_st[-2]) if shared else _I64x2(p_st[0], 0 if single else p_st[1]), axes,
+             (ctypes.c_int32 * axes)(*axis_dims), base, pairing))
+
+
+def _rotary_run(args, q, k, inverse, out, stream):
+    front, behind = args
+    shape, device, q_st = q.shape, q.device, q.stride()
+    k_shape, k_st = (shape, q_st) if k is None else (k.shape, k.stride())
+    if q_st[-1] != 1 or k_st[-1] != 1:
+        raise ValueError("q and k must have d contiguous")
+    with _here(device, stream):
+        if out is None:
+            q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
+        else:
+            q_out, k_out = out[0], None if k is None else out[1]
+            for t, y in ((q, q_out), (k, k_out)):
+                if t is not None and (y.shape != t.shape or y.dtype != t.dtype or y.device != device or y.stride(-1) != 1):
+                    raise ValueError("out must match q and k in shape, type and device, d contiguous")
+        # (the library itself, as in store8 and decode8: the entry points above would ask every argument for its address again)
+        st = lib().sparse_attn_rotary(
+            *front, q.data_ptr(), _row_strides(shape, q_st), q_out.data_ptr(), _row_strides(shape, q_out.stride()),
+            None if k is None else k.data_ptr(), _row_strides(k_shape, k_st), None if k is None else k_out.data_ptr(),
+            None if k is None else _row_strides(k_shape, k_out.stride()), *behind, 1 if inverse else 0,
+            _stream(stream, device))
+    _check("sparse_attn_rotary", st)
+    return q_out, k_out
+
+
 def rotary(q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT, inverse=False, out=None, stream=None):
     """q and k turned by their tokens' places on each axis: (q_out, k_out).
 
@@ -496,43 +542,7 @@ def rotary(q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT,
     token: [b, axes]); ``axis_dims``: the elements of d that each axis owns.
     ``inverse`` turns back, which is also the gradient.  ``out``: (q_out, k_out), the
     inputs themselves allowed."""
-    shape, device, dtype = q.shape, q.device, q.dtype
-    k_shape = shape if k is None else k.shape
-    # (every attribute of a tensor is a call into torch: each is read once)
-    if len(shape) not in (3, 4) or len(k_shape) != len(shape) or k_shape[0] != shape[0] or k_shape[2:] != shape[2:]:
-        raise ValueError("q and k must be [batch, heads, n, d] (or [batch, heads, d]) of one batch, n and d")
-    if device.type != "cuda" or dtype not in _DTYPE_CODES or k is not None and (k.device != device or k.dtype != dtype):
-        raise ValueError("q and k must share type and GPU, in bfloat16 or float32")
-    q_st, k_st = q.stride(), q.stride() if k is None else k.stride()
-    if q_st[-1] != 1 or k_st[-1] != 1:
-        raise ValueError("q and k must have d contiguous")
-    single = len(shape) == 3
-    b, n, d = shape[0], 1 if single else shape[2], shape[-1]
-    axes = len(axis_dims)
-    places, p_st = positions.shape, positions.stride()
-    shared = not single and places in ((n, axes), (1, n, axes))
-    if not shared and places != ((b, axes) if single else (b, n, axes)):
-        raise ValueError("positions must be [n, axes] or [batch, n, axes] (one token: [batch, axes])")
-    if positions.dtype != torch.int32 or positions.device != device or axes > 1 and p_st[-1] != 1:
-        raise ValueError("positions must be int32 with the axes contiguous, on the device of q and k")
-    with _here(device, stream):
-        if out is None:
-            q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
-        else:
-            q_out, k_out = out[0], None if k is None else out[1]
-            for t, y in ((q, q_out), (k, k_out)):
-                if t is not None and (y.shape != t.shape or y.dtype != dtype or y.device != device or y.stride(-1) != 1):
-                    raise ValueError("out must match q and k in shape, type and device, d contiguous")
-        # (the library itself, as in store8 and decode8: the entry points above would ask every argument for its address again)
-        st = lib().sparse_attn_rotary(
-            b, n, shape[1], 0 if k is None else k_shape[1], d, _DTYPE_CODES[dtype], q.data_ptr(), _row_strides(shape, q_st),
-            q_out.data_ptr(), _row_strides(shape, q_out.stride()), None if k is None else k.data_ptr(),
-            _row_strides(k_shape, k_st), None if k is None else k_out.data_ptr(),
-            None if k is None else _row_strides(k_shape, k_out.stride()), positions.data_ptr(),
-            _I64x2(0, p_st[-2]) if shared else _I64x2(p_st[0], 0 if single else p_st[1]), axes,
-            (ctypes.c_int32 * axes)(*axis_dims), base, pairing, 1 if inverse else 0, _stream(stream, device))
-    _check("sparse_attn_rotary", st)
-    return q_out, k_out
+    return _rotary_run(_rotary_args(q, k, positions, axis_dims, base, pairing), q, k, inverse, out, stream)
 
 
 class Rotary(torch.autograd.Function):
@@ -541,21 +551,30 @@ class Rotary(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT, inverse=False):
+        args = _rotary_args(q, k, positions, axis_dims, base, pairing)
         ctx.save_for_backward(positions)
-        ctx.args = (tuple(axis_dims), base, pairing, not inverse)
+        ctx.args, ctx.axis_dims, ctx.inverse = args, tuple(axis_dims), inverse
         ctx.set_materialize_grads(False)
-        return rotary(q, k, positions, axis_dims, base, pairing, inverse)
+        return _rotary_run(args, q, k, inverse, None, None)
 
     @staticmethod
     def backward(ctx, dq, dk):
         (positions,) = ctx.saved_tensors
-        # gradients can come expanded or permuted: rows have to be contiguous, in whole 16-byte pieces
-        grads = [g if g is None or _rows_ok(g) else g.contiguous() for g in (dq, dk)]
+        args, inverse = ctx.args, not ctx.inverse
+        if (dq is not None and dk is not None and dq.is_contiguous() and dk.is_contiguous()
+                and (dq.data_ptr() | dk.data_ptr()) % 16 == 0 and not torch.is_grad_enabled()):
+            # the gradients have the outputs' shapes and type: the forward's arguments hold for them
+            dq, dk = _rotary_run(args, dq, dk, inverse, None, None)
+            return dq, dk, None, None, None, None, None
+        # gradients can be absent, or come expanded, permuted or at an odd address: rows have to be contiguous, in whole
+        # 16-byte pieces
+        grads = [g if g is None or _rows_ok(g) else g.clone(memory_format=torch.contiguous_format) for g in (dq, dk)]
         if grads[0] is None:
             grads.reverse()  # rotary's k is the one that may be absent
         if grads[0] is not None:
+            base, pairing = args[1][-2:]
             turn = Rotary.apply if torch.is_grad_enabled() else rotary
-            grads = list(turn(grads[0], grads[1], positions, *ctx.args))
+            grads = list(turn(grads[0], grads[1], positions, ctx.axis_dims, base, pairing, inverse))
         if dq is None:
             grads.reverse()
         return grads[0], grads[1], None, None, None, None, None

@@ -84,6 +84,8 @@ CASES = [
     (P, IL, 1000, 48, 12, 128, FP, 16, 2, 16),
     (P, IL, 640, 20, 6, 32, BF, 12, 1, 128),       # three subblocks: sets repeat every six heads
     (P, A1, 500, 20, 6, 32, BF, 12, 3, 16),
+    (F, IL, 300, 32, 8, 64, BF, 40, 1, 32),        # forty heads, alternating: two tiles of columns each
+    (P, A2, 400, 32, 16, 32, FP, 70, 2, 16),       # thirty-five heads of one key head, two subblocks
 ]
 
 

@@ -143,6 +143,14 @@ def test_gradients_against_formula_and_differences(halves):
     assert torch.equal(dq_alone, dq)
     (ones,) = torch.autograd.grad(yq.sum(), (q,), retain_graph=True)
     check(ones, torch.ones_like(q), turns, dims, halves, inverse=True)
+    # gradients at an odd address, and permuted
+    yq, yk = sa.Rotary.apply(q, k, places, dims, 10000.0, pairing)
+    odd = [torch.empty(t.numel() + 1, device=t.device)[1:].view(t.shape).copy_(t) for t in w]
+    got = torch.autograd.grad((yq, yk), (q, k), odd, retain_graph=True)
+    assert torch.equal(got[0], dq) and torch.equal(got[1], dk)
+    turned = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in w]
+    got = torch.autograd.grad((yq, yk), (q, k), turned, retain_graph=True)
+    assert torch.equal(got[0], dq) and torch.equal(got[1], dk)
     # the gradient is linear in w: its own gradient is the rotation
     leaf = w[0].clone().requires_grad_()
     (dq,) = torch.autograd.grad(yq, (q,), leaf, create_graph=True)
