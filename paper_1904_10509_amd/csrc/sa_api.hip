@@ -787,7 +787,7 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
     if (st != SA_OK) return st;
     if (max_pos >= capacity) return SA_ERR_INVALID;
     // rows of a (batch, head) are addressed in 16-byte pieces with 32 bits
-    if (cache.ss / 16 * capacity >= (int64_t)1 << 32) return SA_ERR_UNSUPPORTED;
+    if (cache.ss / 16 > (((int64_t)1 << 32) - 1) / capacity) return SA_ERR_UNSUPPORTED;
     if (!positions || !q || !q_strides || !o || !o_strides || !lse) return SA_ERR_INVALID;
     if (!aligned4(positions) || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return SA_ERR_INVALID;
     const int64_t unit = dtype == SA_BF16 ? 8 : 4;  // elements per 16 bytes

@@ -115,7 +115,8 @@ store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
 
     // rows of the block as numbers from its first: new ones are lo .. hi - 1
     const int lo = (int)max64(start - first, 0), hi = (int)min64(end - first, (int64_t)1 << a.c.block_shift);
-    const int64_t from = b * a.xb + h * a.xh + (first - start) * a.xs;  // of the block's first row (before k where lo > 0)
+    // of the block's first row (in front of k where lo > 0: never read)
+    const int64_t from = b * a.xb + h * a.xh + (first - start) * a.xs;
     const int mask = (1 << a.row_shift) - 1;
     Piece<T> x[TENSORS][CH];
     auto is_v = [](int t) { return TENSORS == 1 ? blockIdx.y == 1 : t == 1; };
@@ -195,7 +196,8 @@ hipError_t launch(const StoreArgs& a, int64_t groups, const void* k, const void*
 // A block is 64 to 2,048 pieces of bf16, 128 to 4,096 of fp32: one a thread up to 256 threads, then up
 // to 4 (32 registers for k and v).
 template <typename T>
-hipError_t launch_pieces(const StoreArgs& a, int64_t groups, int pieces, const void* k, const void* v, hipStream_t stream) {
+hipError_t launch_pieces(const StoreArgs& a, int64_t groups, int pieces, const void* k, const void* v,
+                         hipStream_t stream) {
     if constexpr (sizeof(T) == 2)
         if (pieces == 64) return launch<T, 64, 1>(a, groups, k, v, stream);
     if constexpr (sizeof(T) == 4)

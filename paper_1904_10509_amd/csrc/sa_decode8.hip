@@ -143,7 +143,8 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
     __shared__ __align__(16) Lds lds;
     __shared__ float s_m[NWV][kCols], s_top[kCols];
 
-    const int tid = threadIdx.x, lane = tid % 64, w = __builtin_amdgcn_readfirstlane(tid / 64), g = lane / 16, r = lane % 16;
+    const int tid = threadIdx.x, lane = tid % 64, w = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int g = lane / 16, r = lane % 16;
     // the same range of every unit in turn: the workgroups that run together read places far apart
     // (ranges of one unit side by side: 52.8 us against 45.6, loads alone)
     const uint32_t per_split = gridDim.x / a.splits;
@@ -220,7 +221,8 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
             s[t] = zero4();
 #pragma unroll
             for (int f = 0; f < FK; ++f) {
-                const u32x2 k8 = *reinterpret_cast<const u32x2*>(row + (D == 32 ? 8 * g : 64 * (f / 2) + 16 * g + 8 * (f % 2)));
+                const int e = D == 32 ? 8 * g : 64 * (f / 2) + 16 * g + 8 * (f % 2);
+                const u32x2 k8 = *reinterpret_cast<const u32x2*>(row + e);
                 const bf16x8 kf = scaled8(k8[0], k8[1], ks);
 #pragma unroll
                 for (int i = QP - 1; i >= 0; --i) s[t] = mfma_16x16x32(kf, qf[f][i], s[t]);
@@ -254,7 +256,8 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
                 s[t][i] = exp2_fast(fmaf(s[t][i], a.scale_log2, -shift));
                 l += s[t][i];
             }
-        const f32x4 v0 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g]), v1 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g + 4]);
+        const f32x4 v0 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g]);
+        const f32x4 v1 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g + 4]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             s[0][i] *= v0[i];
@@ -363,10 +366,10 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
     }
 }
 
-// One workgroup per (batch, head).  Bound by the latency of reading the ranges' states, so they are read in
-// one round: groups of D threads take every G-th range, eight at a time with a running maximum
-// of their own, and the groups' states meet in LDS (four sequences of 1,048,576, the whole step: 7.4 us; with
-// a common maximum taken first, 8.1).
+// One workgroup per (batch, head).  Bound by the latency of reading the ranges' states, so
+// they are read in one round: groups of D threads take every G-th range, eight at a time
+// with a running maximum of their own, and the groups' states meet in LDS (four sequences
+// of 1,048,576, the whole step: 7.4 us; with a common maximum taken first, 8.1).
 template <int D, typename T, int NT>
 __global__ void __launch_bounds__(NT)
 decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restrict__ o, float* __restrict__ lse) {
@@ -432,15 +435,21 @@ template <int D, typename T>
 hipError_t launch(const Decode8Args& a, int batch, const void* q, void* o, float* lse, float* part, hipStream_t stream) {
     const dim3 grid((unsigned)((int64_t)batch * a.u.units * a.splits)), wg(kWaves * 64);
     if (a.splits == 1) {
-        hipLaunchKernelGGL((decode8_split_kernel<D, T, kWaves, true>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o, lse);
+        hipLaunchKernelGGL((decode8_split_kernel<D, T, kWaves, true>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o,
+                           lse);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((decode8_split_kernel<D, T, kWaves, false>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o, lse);
+    hipLaunchKernelGGL((decode8_split_kernel<D, T, kWaves, false>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o,
+                       lse);
+    // one thread for each of a row's D elements and up to 16 ranges; more ranges, four times the threads (4
+    // sequences of 8 cache heads of 64, 18 ranges: 9.8 -> 9.1 us)
     const dim3 rows((unsigned)(batch * a.heads));
     if (a.splits > 16)
-        hipLaunchKernelGGL((decode8_combine_kernel<D, T, 1024>), rows, dim3(1024), 0, stream, a, (const float*)part, (T*)o, lse);
+        hipLaunchKernelGGL((decode8_combine_kernel<D, T, 1024>), rows, dim3(1024), 0, stream, a, (const float*)part,
+                           (T*)o, lse);
     else
-        hipLaunchKernelGGL((decode8_combine_kernel<D, T, 256>), rows, dim3(256), 0, stream, a, (const float*)part, (T*)o, lse);
+        hipLaunchKernelGGL((decode8_combine_kernel<D, T, 256>), rows, dim3(256), 0, stream, a, (const float*)part,
+                           (T*)o, lse);
     return hipGetLastError();
 }
 
@@ -448,12 +457,12 @@ hipError_t launch(const Decode8Args& a, int batch, const void* q, void* o, float
 //   One range up to 256 keys, two chunks a wave: there is nothing to join (8 heads of 64, 206 keys: one
 //   launch 4.8 us, two ranges 6.7).
 //   Else 128 keys a range, one chunk a wave: the fewer serial steps the better, while there are few
-//   workgroups (8 cache heads of 64, 736 keys: 256 keys a range 7.6 us, 128
-//   7.2; d = 128 fp32, 2,272 keys 11.3 | 9.4).
+//   workgroups (8 cache heads of 64, 736 keys: 256 keys a range 7.6 us, 128 7.2; d = 128 fp32, 2,272
+//   keys 11.3 | 9.4).
 //   From 512 workgroups on (1,024 for d <= 64, whose waves have less on their way; a quarter more before
-//   a wave takes a second chunk) just so many, with longer ranges, as every range costs the join (8 sequences, 4 cache heads, d = 128, 8,416
-//   keys: 2,112 workgroups 25.2, 1,024 20.4, 512 18.9), and at most 128 ranges a unit (one unit,
-//   65,760 keys: 512 ranges 15.1 us, 128 11.6).
+//   a wave takes a second chunk) just so many, with longer ranges, as every range costs the join (8
+//   sequences, 4 cache heads, d = 128, 8,416 keys: 2,112 workgroups 25.2, 1,024 20.4, 512 18.9), and at
+//   most 128 ranges a unit (one unit, 65,760 keys: 512 ranges 15.1 us, 128 11.6).
 //   Where that leaves more than 2,048 keys a range, ranges of about 1,024 (512 for d <= 64): walks of
 //   different speed even out over more than one round (256 units of d = 128, 8,416 keys: 2 ranges
 //   102 us, 8 92.5; 248 of d = 64, about 8,200 keys: 4 48.2, 16 46.6), up to 4,096 results to join or 512

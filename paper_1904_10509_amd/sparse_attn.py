@@ -495,7 +495,8 @@ def _rotary_args(q, k, positions, axis_dims, base, pairing):
     # (every attribute of a tensor is a call into torch: each is read once)
     if len(shape) not in (3, 4) or len(k_shape) != len(shape) or k_shape[0] != shape[0] or k_shape[2:] != shape[2:]:
         raise ValueError("q and k must be [batch, heads, n, d] (or [batch, heads, d]) of one batch, n and d")
-    if device.type != "cuda" or dtype not in _DTYPE_CODES or k is not None and (k.device != device or k.dtype != dtype):
+    if (device.type != "cuda" or dtype not in _DTYPE_CODES
+            or k is not None and (k.device != device or k.dtype != dtype)):
         raise ValueError("q and k must share type and GPU, in bfloat16 or float32")
     single = len(shape) == 3
     b, n, d, axes = shape[0], 1 if single else shape[2], shape[-1], len(axis_dims)
@@ -522,9 +523,10 @@ def _rotary_run(args, q, k, inverse, out, stream):
         else:
             q_out, k_out = out[0], None if k is None else out[1]
             for t, y in ((q, q_out), (k, k_out)):
-                if t is not None and (y.shape != t.shape or y.dtype != t.dtype or y.device != device or y.stride(-1) != 1):
+                if t is not None and (y.shape != t.shape or y.dtype != t.dtype or y.device != device
+                                      or y.stride(-1) != 1):
                     raise ValueError("out must match q and k in shape, type and device, d contiguous")
-        # (the library itself, as in store8 and decode8: the entry points above would ask every argument for its address again)
+        # (the library itself, as in store8 and decode8: the entry points above would look at every argument again)
         st = lib().sparse_attn_rotary(
             *front, q.data_ptr(), _row_strides(shape, q_st), q_out.data_ptr(), _row_strides(shape, q_out.stride()),
             None if k is None else k.data_ptr(), _row_strides(k_shape, k_st), None if k is None else k_out.data_ptr(),
@@ -620,7 +622,8 @@ def build_cache8(batch, kv_heads, capacity, d, block=64, device="cuda"):
     """An empty 8-bit cache.  A token's key and value lie side by side: the patterns that gather single tokens read
     them in one piece."""
     kv = torch.empty((batch, kv_heads, capacity, 2, d), dtype=torch.float8_e4m3fn, device=device)
-    scales = torch.zeros((2, batch, kv_heads, -(-capacity // block)), dtype=torch.float32, device=device)  # 0: nothing yet
+    # scales of 0: nothing is held yet
+    scales = torch.zeros((2, batch, kv_heads, -(-capacity // block)), dtype=torch.float32, device=device)
     return Cache8(kv[..., 0, :], kv[..., 1, :], scales[0], scales[1], block)
 
 
@@ -629,7 +632,8 @@ def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
     counts[b] of sequence b at positions start[b], ... (int32 [b] on the device; None: 0, and all of them)."""
     shape, st, device, dtype = k.shape, k.stride(), k.device, k.dtype
     if len(shape) not in (3, 4) or v.shape != shape or v.stride() != st or v.dtype != dtype or v.device != device:
-        raise ValueError("k and v must be [batch, kv_heads, n_new, d] (or [batch, kv_heads, d]) of one layout, type and GPU")
+        raise ValueError("k and v must be [batch, kv_heads, n_new, d] (or [batch, kv_heads, d]) of one layout, type and "
+                         "GPU")
     if device.type != "cuda" or dtype not in _DTYPE_CODES or st[-1] != 1:
         raise ValueError("k and v must be bfloat16 or float32 on the GPU, d contiguous")
     b, h, d = shape[0], shape[1], shape[-1]

@@ -90,6 +90,7 @@ DECODE = dict(pos=FAKE, max_pos=99, l=16, c=0, pattern=sa.SA_STRIDED, mode=sa.SA
     (dict(o=None), INV), (dict(os=None), INV), (dict(os=longs(0, 64)), INV), (dict(os=longs(256, 56)), INV),
     (dict(os=longs(256, 68)), INV), (dict(lse=None), INV), (dict(lse=FAKE + 2), INV), (dict(ws=None), INV), (dict(ws=FAKE + 8), INV),
     (dict(wsb=0), SMALL), (dict(batch=2 ** 20, heads=8), UNS), (dict(capacity=2 ** 31 - 1), UNS),
+    (dict(cs=longs(0, 0, 2 ** 62)), UNS),
 ])
 def test_decode8_refusals(L, over, expect):
     assert L.sparse_attn_decode8(*dict(DECODE, **over).values()) == expect
