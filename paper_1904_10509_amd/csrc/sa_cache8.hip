@@ -186,10 +186,15 @@ store_kernel(StoreArgs a, const T* __restrict__ k, const T* __restrict__ v) {
 template <typename T, int NT, int CH>
 hipError_t launch(const StoreArgs& a, int64_t groups, const void* k, const void* v, hipStream_t stream) {
     const T *kt = (const T*)k, *vt = (const T*)v;
-    if (groups < kFewGroups)
-        hipLaunchKernelGGL((store_kernel<T, NT, CH, 1>), dim3((unsigned)groups, 2), dim3(NT), 0, stream, a, kt, vt);
-    else
-        hipLaunchKernelGGL((store_kernel<T, NT, CH, 2>), dim3((unsigned)groups), dim3(NT), 0, stream, a, kt, vt);
+    // (1,024 threads with both would have a compute unit to themselves: 8 x 3,000 tokens, 8 heads of 128, fp32, blocks
+    // of 128 59.8 us, apart 47.6)
+    if constexpr (NT < 1024) {
+        if (groups >= kFewGroups) {
+            hipLaunchKernelGGL((store_kernel<T, NT, CH, 2>), dim3((unsigned)groups), dim3(NT), 0, stream, a, kt, vt);
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((store_kernel<T, NT, CH, 1>), dim3((unsigned)groups, 2), dim3(NT), 0, stream, a, kt, vt);
     return hipGetLastError();
 }
 
