@@ -353,7 +353,7 @@ int sparse_attn_rotary(int32_t batch, int64_t n, int32_t q_heads, int32_t k_head
  *   k_scale, v_scale  [batch, kv_heads, ceil(capacity / scale_block)] contiguous fp32
  *   scale_block       in {16, 32, 64, 128};  capacity in [1, 2^31 - 1]
  *
- * sparse_attn_cache8_store writes n_new new keys and values of every sequence
+ * sparse_attn_cache8_store writes n_new >= 1 new keys and values of every sequence
  * (n_new = 1: one generated token), [batch, kv_heads, n_new, d_head] with element
  * strides kv_strides[0..2] for both, d contiguous, bf16 or fp32 (dtype):
  * sequence b's first counts[b] of them go to positions start[b], start[b] + 1, ...

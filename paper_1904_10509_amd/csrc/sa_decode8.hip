@@ -67,11 +67,11 @@ struct Decode8Args {
     float scale_log2;
 };
 
+// Factor of a state with maximum m (a q . k, unscaled) in a sum relative to mx >= m; m = -inf
+// is the empty state.
 __device__ inline float weight(float m, float mx, float scale) {
     return m == -INFINITY ? 0.f : exp2_fast((m - mx) * scale);
 }
-// Factor of a state with maximum m in a sum relative to mx >= m; m = -inf is the empty state.
-__device__ inline float weight(float m, float mx) { return m == -INFINITY ? 0.f : exp2_fast(m - mx); }
 
 __device__ inline void put_nan(uint16_t* dst) { *dst = 0x7fc0; }
 __device__ inline void put_nan(float* dst) { *reinterpret_cast<uint32_t*>(dst) = 0x7fc00000u; }
@@ -248,12 +248,13 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
                 for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
             m = mx;
         }
-        const float shift = m * a.scale_log2;
+        // (the difference first: the largest score has a weight of 1 and its neighbours' are right however
+        // large both are; scaling before would lose 2^-24 of the scores themselves)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[t][i] = exp2_fast(fmaf(s[t][i], a.scale_log2, -shift));
+                s[t][i] = exp2_fast((s[t][i] - m) * a.scale_log2);
                 l += s[t][i];
             }
         const f32x4 v0 = *reinterpret_cast<const f32x4*>(&mine.vs[8 * g]);
@@ -333,7 +334,7 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
         }
         if (g == 0) {
             lds.join.l[w][r] = l * wt;
-            if (w == 0) s_top[r] = top * a.scale_log2;
+            if (w == 0) s_top[r] = top;
         }
     }
     __syncthreads();
@@ -353,7 +354,7 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
             else put(dst, sum * (total > 0.f ? 1.f / total : 0.f));
             if (e == 0) {
                 if (beyond) put_nan(lse + row);
-                else lse[row] = total > 0.f ? (s_top[c] + __log2f(total)) / kLog2e : -INFINITY;
+                else lse[row] = total > 0.f ? (s_top[c] * a.scale_log2 + __log2f(total)) / kLog2e : -INFINITY;
             }
         } else {
             float* dst = part + (row * a.splits + split) * (D + 2);
@@ -392,13 +393,13 @@ decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restr
         float mx = m;
 #pragma unroll
         for (int u = 0; u < U; ++u) mx = fmaxf(mx, ms[u]);
-        const float old = weight(m, mx);
+        const float old = weight(m, mx, a.scale_log2);
         l *= old;
         x *= old;
         m = mx;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float wt = s0 + u * G < a.splits ? weight(ms[u], mx) : 0.f;
+            const float wt = s0 + u * G < a.splits ? weight(ms[u], mx, a.scale_log2) : 0.f;
             l = fmaf(ls[u], wt, l);
             x = fmaf(xs[u], wt, x);
         }
@@ -416,7 +417,7 @@ decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restr
         x = l = 0.f;
 #pragma unroll
         for (int t = 0; t < G; ++t) {
-            const float wt = weight(s_m[t], m);
+            const float wt = weight(s_m[t], m, a.scale_log2);
             x = fmaf(s_x[t][tid], wt, x);
             l = fmaf(s_l[t], wt, l);
         }
@@ -426,7 +427,7 @@ decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restr
             if (tid == 0) put_nan(lse + row);
         } else {  // no key: o = 0, lse = -inf
             put(dst, x * (l > 0.f ? 1.f / l : 0.f));
-            if (tid == 0) lse[row] = l > 0.f ? (m + __log2f(l)) / kLog2e : -INFINITY;
+            if (tid == 0) lse[row] = l > 0.f ? (m * a.scale_log2 + __log2f(l)) / kLog2e : -INFINITY;
         }
     }
 }

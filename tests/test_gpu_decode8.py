@@ -137,6 +137,25 @@ def test_large_and_small_scores():
             check(o, lse, q, values, at, 50, 0, S, MG, 1.0)
 
 
+def test_equal_keys_of_large_scores():
+    """Keys that are all alike, with scores in the thousands: every weight is the same to the bit, whatever chunk, wave or
+    range it falls into, so the output is the mean of the values: off by the sum's own roundings, count 2^-24 of the mean
+    |v|, three at the end, and an fp32 weight's third piece (2^-24)."""
+    dev, d, capacity = device(), 64, 3000
+    cache = sa.build_cache8(1, 1, capacity, d, 64, device=dev)
+    k = torch.full((1, 1, capacity, d), 13.0, dtype=BF, device=dev)
+    v = torch.randn((1, 1, capacity, d), generator=torch.Generator().manual_seed(1)).to(BF).to(dev)
+    sa.store8(cache, k, v)
+    q = torch.full((1, 2, d), 5.1, device=dev)
+    for pos in (0, 40, 250, 700, 2999):
+        o, lse = sa.decode8(q, cache, torch.tensor([pos], dtype=torch.int32, device=dev), 1, 0, S, MG, softmax_scale=1.0)
+        torch.cuda.synchronize()
+        values = (ref.VALUES[cache.v.view(torch.uint8).cpu().numpy()]
+                  * to64(cache.v_scale)[:, :, np.arange(capacity) // 64, None])[0, 0, :pos + 1]
+        lim = (pos + 1 + 5) * 2.0 ** -24 * np.abs(values).mean(axis=0)
+        assert np.all(np.abs(to64(o) - values.mean(axis=0)) <= lim), pos
+
+
 def test_layouts_outputs_and_workspace():
     """Keys and values apart in wide rows, query and output views, a caller's workspace: the bits of the plain call."""
     dev, d, l, c = device(), 64, 32, 8
@@ -163,6 +182,28 @@ def test_layouts_outputs_and_workspace():
     got = sa.decode8(same, shared, torch.tensor([at[0]] * 2, dtype=torch.int32, device=dev), l, c, F, MG)
     assert torch.equal(got[0], want[0][:1].expand_as(got[0])) and torch.equal(got[1], want[1][:1].expand_as(got[1]))
     assert torch.all(out[..., :d] == 5) and torch.all(out[..., 2 * d:] == 5) and torch.all(ws[max(need, 16):] == 255)
+
+
+@pytest.mark.parametrize("exponent", [-100, -7, 0, 3, 100])
+def test_every_code(exponent):
+    """One key alone: the output is its value, code times scale, to the bit (fp32: the weight is 1), for every finite code;
+    with one-hot queries the log-sum-exp is the key's element times the softmax scale, to 2^-20 (two changes of base)."""
+    dev, d = device(), 128
+    codes = torch.arange(256, dtype=torch.uint8)
+    codes[(codes & 127) == 127] = 3  # NaN
+    cache = sa.build_cache8(2, 1, 1, d, 16, device=dev)
+    for t in (cache.k, cache.v):
+        t.copy_(codes.reshape(2, 1, 1, d).view(torch.float8_e4m3fn))
+    cache.k_scale.fill_(2.0 ** exponent)
+    cache.v_scale.fill_(2.0 ** exponent)
+    want = ref.VALUES[codes.numpy()].reshape(2, 1, d) * 2.0 ** exponent
+    q = torch.eye(d).expand(2, d, d)
+    for dtype in (FP, BF):
+        o, lse = sa.decode8(q.to(dtype).to(dev), cache, torch.zeros(2, dtype=torch.int32, device=dev), 1, 0, S, MG,
+                            softmax_scale=0.5)
+        torch.cuda.synchronize()
+        assert np.array_equal(to64(o), np.broadcast_to(want, (2, d, d)))  # four bits: exact in bf16 as well
+        assert np.all(np.abs(to64(lse) - 0.5 * want[:, 0]) <= 2.0 ** -20 * np.abs(0.5 * want[:, 0]))
 
 
 def test_positions_of_any_value():
