@@ -488,8 +488,8 @@ def grid_positions(shape, device="cuda"):
     return torch.stack([a.reshape(-1) for a in axes], dim=1)
 
 
-def _rotary_args(q, k, positions, axis_dims, base, pairing):
-    """What a call on tensors of these shapes passes in front of them and behind them, checked."""
+def _rotary_args(q, k, axis_dims, base, pairing):
+    """What a call on tensors of these shapes passes in front of the tensors, and what behind the positions, checked."""
     shape, device, dtype = q.shape, q.device, q.dtype
     k_shape = shape if k is None else k.shape
     # (every attribute of a tensor is a call into torch: each is read once)
@@ -498,25 +498,32 @@ def _rotary_args(q, k, positions, axis_dims, base, pairing):
     if (device.type != "cuda" or dtype not in _DTYPE_CODES
             or k is not None and (k.device != device or k.dtype != dtype)):
         raise ValueError("q and k must share type and GPU, in bfloat16 or float32")
-    single = len(shape) == 3
-    b, n, d, axes = shape[0], 1 if single else shape[2], shape[-1], len(axis_dims)
-    places, p_st = positions.shape, positions.stride()
+    n, axes = 1 if len(shape) == 3 else shape[2], len(axis_dims)
+    return ((shape[0], n, shape[1], 0 if k is None else k_shape[1], shape[-1], _DTYPE_CODES[dtype]),
+            (axes, (ctypes.c_int32 * axes)(*axis_dims), base, pairing))
+
+
+def _rotary_places(positions, shape, axes, device):
+    """Address and strides of the positions of tokens [batch, heads, n, d] or [batch, heads, d], checked."""
+    single, b = len(shape) == 3, shape[0]
+    n = 1 if single else shape[2]
+    places, st = positions.shape, positions.stride()
     shared = not single and places in ((n, axes), (1, n, axes))
     if not shared and places != ((b, axes) if single else (b, n, axes)):
         raise ValueError("positions must be [n, axes] or [batch, n, axes] (one token: [batch, axes])")
-    if positions.dtype != torch.int32 or positions.device != device or axes > 1 and p_st[-1] != 1:
+    if positions.dtype != torch.int32 or positions.device != device or axes > 1 and st[-1] != 1:
         raise ValueError("positions must be int32 with the axes contiguous, on the device of q and k")
-    return ((b, n, shape[1], 0 if k is None else k_shape[1], d, _DTYPE_CODES[dtype]),
-            (positions.data_ptr(), _I64x2(0, p_st[-2]) if shared else _I64x2(p_st[0], 0 if single else p_st[1]), axes,
-             (ctypes.c_int32 * axes)(*axis_dims), base, pairing))
+    return positions.data_ptr(), _I64x2(0, st[-2]) if shared else _I64x2(st[0], 0 if single else st[1])
 
 
-def _rotary_run(args, q, k, inverse, out, stream):
+def _rotary_run(args, q, k, positions, inverse, out, stream):
     front, behind = args
     shape, device, q_st = q.shape, q.device, q.stride()
     k_shape, k_st = (shape, q_st) if k is None else (k.shape, k.stride())
     if q_st[-1] != 1 or k_st[-1] != 1:
         raise ValueError("q and k must have d contiguous")
+    # (of the tensor that is read now: an address is never kept from one call for the next)
+    places = _rotary_places(positions, shape, behind[0], device)
     with _here(device, stream):
         if out is None:
             q_out, k_out = torch.empty_like(q), None if k is None else torch.empty_like(k)
@@ -530,7 +537,7 @@ def _rotary_run(args, q, k, inverse, out, stream):
         st = lib().sparse_attn_rotary(
             *front, q.data_ptr(), _row_strides(shape, q_st), q_out.data_ptr(), _row_strides(shape, q_out.stride()),
             None if k is None else k.data_ptr(), _row_strides(k_shape, k_st), None if k is None else k_out.data_ptr(),
-            None if k is None else _row_strides(k_shape, k_out.stride()), *behind, 1 if inverse else 0,
+            None if k is None else _row_strides(k_shape, k_out.stride()), *places, *behind, 1 if inverse else 0,
             _stream(stream, device))
     _check("sparse_attn_rotary", st)
     return q_out, k_out
@@ -544,7 +551,7 @@ def rotary(q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT,
     token: [b, axes]); ``axis_dims``: the elements of d that each axis owns.
     ``inverse`` turns back, which is also the gradient.  ``out``: (q_out, k_out), the
     inputs themselves allowed."""
-    return _rotary_run(_rotary_args(q, k, positions, axis_dims, base, pairing), q, k, inverse, out, stream)
+    return _rotary_run(_rotary_args(q, k, axis_dims, base, pairing), q, k, positions, inverse, out, stream)
 
 
 class Rotary(torch.autograd.Function):
@@ -553,20 +560,20 @@ class Rotary(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT, inverse=False):
-        args = _rotary_args(q, k, positions, axis_dims, base, pairing)
+        args = _rotary_args(q, k, axis_dims, base, pairing)
         ctx.save_for_backward(positions)
         ctx.args, ctx.axis_dims, ctx.inverse = args, tuple(axis_dims), inverse
         ctx.set_materialize_grads(False)
-        return _rotary_run(args, q, k, inverse, None, None)
+        return _rotary_run(args, q, k, positions, inverse, None, None)
 
     @staticmethod
     def backward(ctx, dq, dk):
-        (positions,) = ctx.saved_tensors
+        (positions,) = ctx.saved_tensors  # what a saved-tensor hook made of them, at another address perhaps
         args, inverse = ctx.args, not ctx.inverse
         if (dq is not None and dk is not None and dq.is_contiguous() and dk.is_contiguous()
                 and (dq.data_ptr() | dk.data_ptr()) % 16 == 0 and not torch.is_grad_enabled()):
-            # the gradients have the outputs' shapes and type: the forward's arguments hold for them
-            dq, dk = _rotary_run(args, dq, dk, inverse, None, None)
+            # the gradients have the outputs' shapes and type: what the forward's call said of those holds for them
+            dq, dk = _rotary_run(args, dq, dk, positions, inverse, None, None)
             return dq, dk, None, None, None, None, None
         # gradients can be absent, or come expanded, permuted or at an odd address: rows have to be contiguous, in whole
         # 16-byte pieces
