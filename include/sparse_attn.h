@@ -397,7 +397,9 @@ int sparse_attn_cache8_store(int32_t batch, int32_t kv_heads, int64_t n_new, int
  *   lse        [batch, heads] contiguous fp32, natural log
  * Cache arguments as for sparse_attn_cache8_store (scales powers of two).  Codes
  * times scales are exact in bf16; q . k is accumulated in fp32 from unrounded
- * terms.  Rows outside the set are never read into a result.  Every base
+ * terms.  Rows outside the set are never read into a result.  A NaN among the attended keys
+ * or in a query makes that row's o and lse NaN (-inf is a row without a key alone), one among
+ * the values its element of o.  Every base
  * address 16-byte aligned (scales and positions 4), cache strides multiples
  * of 16, strides of q and o multiples of 16 bytes, the cache's token stride >=
  * d_head.  Sequences or heads may share rows of the cache (a stride of 0).

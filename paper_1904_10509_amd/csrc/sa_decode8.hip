@@ -73,6 +73,10 @@ __device__ inline float weight(float m, float mx, float scale) {
     return m == -INFINITY ? 0.f : exp2_fast((m - mx) * scale);
 }
 
+// Whether a row's sum of weights (>= 0, or NaN) says that it has no key.  By its bits: the build lets comparisons
+// assume that there is no NaN, and a NaN score must not pass for an empty row.
+__device__ inline bool no_key(float total) { return __float_as_uint(total) == 0; }
+
 __device__ inline void put_nan(uint16_t* dst) { *dst = 0x7fc0; }
 __device__ inline void put_nan(float* dst) { *reinterpret_cast<uint32_t*>(dst) = 0x7fc00000u; }
 template <typename T>
@@ -351,10 +355,10 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
         if constexpr (DIRECT) {
             T* dst = o + b * a.osb + head * a.osh + e;
             if (beyond) put_nan(dst);
-            else put(dst, sum * (total > 0.f ? 1.f / total : 0.f));
+            else put(dst, sum * (no_key(total) ? 0.f : 1.f / total));
             if (e == 0) {
                 if (beyond) put_nan(lse + row);
-                else lse[row] = total > 0.f ? (s_top[c] * a.scale_log2 + __log2f(total)) / kLog2e : -INFINITY;
+                else lse[row] = no_key(total) ? -INFINITY : (s_top[c] * a.scale_log2 + __log2f(total)) / kLog2e;
             }
         } else {
             float* dst = part + (row * a.splits + split) * (D + 2);
@@ -426,8 +430,8 @@ decode8_combine_kernel(Decode8Args a, const float* __restrict__ part, T* __restr
             put_nan(dst);
             if (tid == 0) put_nan(lse + row);
         } else {  // no key: o = 0, lse = -inf
-            put(dst, x * (l > 0.f ? 1.f / l : 0.f));
-            if (tid == 0) lse[row] = l > 0.f ? (m * a.scale_log2 + __log2f(l)) / kLog2e : -INFINITY;
+            put(dst, x * (no_key(l) ? 0.f : 1.f / l));
+            if (tid == 0) lse[row] = no_key(l) ? -INFINITY : (m * a.scale_log2 + __log2f(l)) / kLog2e;
         }
     }
 }
