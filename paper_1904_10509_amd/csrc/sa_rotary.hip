@@ -9,12 +9,11 @@
 //
 // The angle in turns is p f / (2 pi) modulo 1.  With F = f / (2 pi) in units of
 // 2^-64 turns, the low 64 bits of the integer product p F are that fraction, off by
-// p times F's own error (2^-60.3, so 2^-29 turns at the furthest place) and with no range
+// p times F's own error (sa_turns.h: 2^-29.9 turns at the furthest place) and with no range
 // reduction: places of millions lose nothing.  Its upper 32 bits, read as signed, are the turn in [-1/2, 1/2).
-#include <math.h>
-
 #include "sa_internal.h"
 #include "sa_mfma.h"
+#include "sa_turns.h"
 
 namespace sa {
 
@@ -201,14 +200,11 @@ hipError_t rotary_launch(const RotaryCall& c, hipStream_t stream) {
     a.tokens = c.n * c.batch;
     a.axes = c.axes;
     a.sign = c.inverse ? -1.f : 1.f;
-    // F by repeated products in extended precision (64 bits of mantissa): pair t is off by about
-    // 2 t 2^-64 f_t turns, which falls with f_t: 13 units of 2^-64 at most (base 1.5, 64 pairs).
     int pair = 0;
     int w = 8;
     for (int x = 0; x < c.axes; ++x) {
-        const long double step = powl((long double)c.base, -2.0L / c.dims[x]);
-        long double f = 0x1p64L / 6.283185307179586476925286766559L;
-        for (int t = 0; t < c.dims[x] / 2; ++t, f *= step) a.turn[pair++] = (uint64_t)(f + 0.5L);
+        turn_units(c.base, c.dims[x], a.turn + pair);
+        pair += c.dims[x] / 2;
         a.end[x] = 2 * pair;
         while ((c.dims[x] / 2) % w != 0) w /= 2;
     }
