@@ -326,8 +326,9 @@ int sparse_attn_decode(int64_t pos, int32_t stride_l, int32_t summary_c, int32_t
  *                  any int32, negative ones included
  *   n              1 <= n < 2^31 (n = 1: the new token of every sequence)
  *   n_axes         1 .. 4
- * Angles are exact to 2^-29 turns at every place; products in fp32, one rounding at
- * the end.  Every base address 16-byte aligned and every stride of q, k and the
+ * fp32: angles are within 2^-27 turns at every place, their sines and cosines within a unit
+ * in the last place.  bf16: sines and cosines are within 2^-22.  Products in fp32, one
+ * rounding at the end.  Every base address 16-byte aligned and every stride of q, k and the
  * outputs a multiple of 16 bytes, token strides >= d_head, rows of an output apart; positions 4-byte
  * aligned, strides >= 0.  d_head in {32, 64, 128}; batch * n < 2^33 and at most
  * 65,535 heads of each tensor, else SA_ERR_UNSUPPORTED.

@@ -63,11 +63,19 @@ __device__ inline void set_element(typename Piece<T, N>::type& v, int e, float x
     else v[e] = (T)x;
 }
 
-// Sine and cosine of an angle in units of 2^-32 turns.  fp32 results take the library's
-// (2^-23); for bf16 results, which round to 2^-8, the hardware's instructions, whose argument
-// is in turns (one token 3.4 -> 2.8 us; 2 sequences of 12,288, both directions, 45.5 -> 42.1).
+// Sine and cosine of an angle in units of 2^-32 turns.  fp32 results take the library's, within
+// a unit in the last place, of what is left of the angle behind its nearest quarter turn.  That is taken off
+// in integers: as a float, a whole half turn is off by up to 2^-26 turns, more than the last place of its
+// sine, and an eighth by 2^-28.  For bf16 results, which round to 2^-8, the hardware's instructions, whose
+// argument is in turns: off by 2^-22.3 at most (measured over 3e7 angles; one token 3.4 -> 2.8 us;
+// 2 sequences of 12,288, both directions, 45.5 -> 42.1).
 __device__ inline void turn_sincos(int32_t turn, float* s, float* c, const float*) {
-    sincospif((float)turn * 0x1p-31f, s, c);
+    const uint32_t quarter = ((uint32_t)turn + 0x20000000u) >> 30;
+    float a, b;
+    sincospif((float)(int32_t)((uint32_t)turn - (quarter << 30)) * 0x1p-31f, &a, &b);
+    const float x = quarter & 1 ? b : a, y = quarter & 1 ? a : b;
+    *s = quarter & 2 ? -x : x;
+    *c = (quarter + 1) & 2 ? -y : y;
 }
 __device__ inline void turn_sincos(int32_t turn, float* s, float* c, const __bf16*) {
     const float x = (float)turn * 0x1p-32f;
