@@ -223,13 +223,22 @@ decode8_split_kernel(Decode8Args a, const T* __restrict__ q, float* __restrict__
             const uint8_t* row = mine.rows + u * WaveLds<D>::kPitch;
             const float ks = mine.ks[u];
             s[t] = zero4();
+            // what the smaller pieces of an fp32 query add, summed apart: one by one into the whole sum, each of these
+            // products would round it once more (8 of 12 at d = 128; error of o against 64 bits 2.9e-7 -> 1.5e-7, the
+            // time the same)
+            f32x4 low = zero4();
 #pragma unroll
             for (int f = 0; f < FK; ++f) {
                 const int e = D == 32 ? 8 * g : 64 * (f / 2) + 16 * g + 8 * (f % 2);
                 const u32x2 k8 = *reinterpret_cast<const u32x2*>(row + e);
                 const bf16x8 kf = scaled8(k8[0], k8[1], ks);
 #pragma unroll
-                for (int i = QP - 1; i >= 0; --i) s[t] = mfma_16x16x32(kf, qf[f][i], s[t]);
+                for (int i = QP - 1; i > 0; --i) low = mfma_16x16x32(kf, qf[f][i], low);
+                s[t] = mfma_16x16x32(kf, qf[f][0], s[t]);
+            }
+            if constexpr (QP > 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[t][i] += low[i];
             }
         }
         if (first + kChunk > t1) {
