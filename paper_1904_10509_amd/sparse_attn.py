@@ -452,6 +452,7 @@ def decode(q, k_cache, v_cache, pos, stride_l, summary_c, pattern, head_mode, so
 # ---------------------------------------------------------------------------
 _SAME = contextlib.nullcontext()
 _I64x2, _I64x3 = ctypes.c_int64 * 2, ctypes.c_int64 * 3
+_CODE_TYPES = (torch.float8_e4m3fn, torch.uint8)
 _DTYPE_CODES = {torch.bfloat16: SA_BF16, torch.float32: SA_F32}
 
 
@@ -611,8 +612,11 @@ class Cache8:
         """Batch, heads, capacity and strides, checked."""
         k, v, k_scale, v_scale = self.k, self.v, self.k_scale, self.v_scale
         shape, st = k.shape, k.stride()
-        if len(shape) != 4 or k.element_size() != 1 or v.shape != shape or v.stride() != st or v.dtype != k.dtype:
-            raise ValueError("the cache's k and v must be 8-bit [batch, kv_heads, capacity, d] tensors of one layout")
+        # (other types of eight bits have other values for the codes)
+        if k.dtype not in _CODE_TYPES or v.dtype not in _CODE_TYPES:
+            raise ValueError("the cache's k and v must be float8_e4m3fn or uint8 tensors")
+        if len(shape) != 4 or v.shape != shape or v.stride() != st:
+            raise ValueError("the cache's k and v must be [batch, kv_heads, capacity, d] tensors of one layout")
         if shape[3] != d or st[3] != 1:
             raise ValueError("the cache must have the d of the tensors, contiguous")
         b, h, capacity, _ = shape

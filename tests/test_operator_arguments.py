@@ -1,0 +1,77 @@
+"""What the binding takes and refuses around the 8-bit cache, without a GPU: the launches are recorded in place of being made."""
+import contextlib
+import ctypes
+
+import pytest
+import torch
+
+from paper_1904_10509_amd import sparse_attn as sa
+
+GPU = torch.device("cuda", 0)
+B, KV, CAP, D, T = 2, 4, 100, 64, 32
+
+
+class OnGpu(torch.Tensor):
+    """A tensor in host memory that the binding takes for one on the GPU."""
+
+    @property
+    def device(self):
+        return GPU
+
+
+class Library:
+    """Records the calls by name; a decoding step asks for a workspace of 4,096 bytes."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            if name == "sparse_attn_decode8_workspace_size":
+                args[-1]._obj.value = 4096
+            else:
+                self.calls.append((name, args))
+            return sa.SA_OK
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    got = Library()
+    monkeypatch.setattr(sa, "lib", lambda: got)
+    monkeypatch.setattr(sa, "_here", lambda device, stream: contextlib.nullcontext())
+    monkeypatch.setattr(sa, "_stream", lambda stream, device: 0)
+    return got
+
+
+def gpu(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+def cache(dtype=torch.float8_e4m3fn):
+    c = sa.build_cache8(B, KV, CAP, D, T, device="cpu")
+    return sa.Cache8(*(t.as_subclass(OnGpu) for t in (c.k.view(dtype), c.v.view(dtype), c.k_scale, c.v_scale)), T)
+
+
+def decode(c, **over):
+    args = dict(q=gpu(B, KV, D), cache=c, positions=gpu(B, dtype=torch.int32), stride_l=16, summary_c=0,
+                pattern=sa.SA_STRIDED, head_mode=sa.SA_MODE_MERGED)
+    args.update(over)
+    return sa.decode8(**args)
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e4m3fn, torch.uint8])
+def test_cache_types(library, dtype):
+    sa.store8(cache(dtype), gpu(B, KV, 5, D), gpu(B, KV, 5, D))
+    decode(cache(dtype))
+    assert [name for name, _ in library.calls] == ["sparse_attn_cache8_store", "sparse_attn_decode8"]
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.int8])
+def test_other_types_of_eight_bits_are_refused(library, dtype):
+    """Their values are not those of the codes that the cache holds."""
+    with pytest.raises(ValueError, match="float8_e4m3fn or uint8"):
+        sa.store8(cache(dtype), gpu(B, KV, 5, D), gpu(B, KV, 5, D))
+    with pytest.raises(ValueError, match="float8_e4m3fn or uint8"):
+        decode(cache(dtype))
+    assert not library.calls
