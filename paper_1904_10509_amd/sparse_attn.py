@@ -699,8 +699,8 @@ def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode
             workspace = q.new_empty(need, dtype=torch.uint8)
         else:
             need = workspace.numel() * workspace.element_size()
-            if workspace.device != device:
-                raise ValueError("workspace must be on q's device")
+            if workspace.device != device or not workspace.is_contiguous():
+                raise ValueError("workspace must be contiguous, on q's device")
         status = lib().sparse_attn_decode8(
             positions.data_ptr(), max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, code, q.data_ptr(),
             _I64x2(st[0] if b > 1 else 0, st[1] if h > 1 else 0), cache.k.data_ptr(), cache.v.data_ptr(), cache_strides,

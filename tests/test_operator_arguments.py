@@ -75,3 +75,14 @@ def test_other_types_of_eight_bits_are_refused(library, dtype):
     with pytest.raises(ValueError, match="float8_e4m3fn or uint8"):
         decode(cache(dtype))
     assert not library.calls
+
+
+def test_workspace_in_pieces_is_refused(library):
+    """The library writes as many bytes as the workspace has elements, one behind the other."""
+    room = torch.zeros(16, dtype=torch.uint8).as_subclass(OnGpu)
+    for bad in (room[:1].expand(8192), gpu(16384, dtype=torch.uint8)[::2], gpu(64, 128, dtype=torch.uint8).t()):
+        with pytest.raises(ValueError, match="contiguous"):
+            decode(cache(), workspace=bad)
+    assert not library.calls
+    decode(cache(), workspace=gpu(64, 128, dtype=torch.uint8))
+    assert library.calls[0][1][-2] == 8192
