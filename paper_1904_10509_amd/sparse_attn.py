@@ -16,6 +16,7 @@ import os
 from dataclasses import dataclass
 
 import torch
+from torch.autograd.graph import increment_version
 
 # SPARSE_ATTN_LIB names another build of the same sources to load instead (the
 # sanitizer test loads one whose host code is built with ASan and UBSan).
@@ -299,6 +300,7 @@ def sparse_attn_cache8_store(batch, kv_heads, n_new, d_head, dtype, k, v, kv_str
                                         _ptr(counts), capacity, scale_block, _ptr(k_cache), _ptr(v_cache),
                                         cache_strides, _ptr(k_scale), _ptr(v_scale), _stream(stream, k.device))
     _check("sparse_attn_cache8_store", st)
+    increment_version((cache.k, cache.v, cache.k_scale, cache.v_scale))
 
 
 def sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads, d_head,
@@ -541,6 +543,8 @@ def _rotary_run(args, q, k, positions, inverse, out, stream):
             None if k is None else _row_strides(k_shape, k_out.stride()), *places, *behind, 1 if inverse else 0,
             _stream(stream, device))
     _check("sparse_attn_rotary", st)
+    if out is not None:  # written behind torch's back: a graph that saved these has to know
+        increment_version((q_out,) if k is None else (q_out, k_out))
     return q_out, k_out
 
 
@@ -662,6 +666,7 @@ def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
             None if counts is None else counts.data_ptr(), capacity, cache.block, cache.k.data_ptr(), cache.v.data_ptr(),
             cache_strides, cache.k_scale.data_ptr(), cache.v_scale.data_ptr(), _stream(stream, device))
     _check("sparse_attn_cache8_store", st)
+    increment_version((cache.k, cache.v, cache.k_scale, cache.v_scale))
 
 
 def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode, max_pos=None, softmax_scale=None,
@@ -678,6 +683,7 @@ def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode
         raise ValueError("q must have the cache's batch and a multiple of its heads")
     _check_ints("positions", positions, b, device)
     max_pos = capacity - 1 if max_pos is None else max_pos
+    given = [t for t in (out, lse) if t is not None]  # written behind torch's back
     code = _DTYPE_CODES[dtype]
     with _here(device, stream):
         if out is None:
@@ -709,6 +715,8 @@ def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode
             _I64x2(o_st[0] if b > 1 else 0, o_st[1] if h > 1 else 0), lse.data_ptr(), workspace.data_ptr(), need,
             _stream(stream, device))
     _check("sparse_attn_decode8", status)
+    if given:
+        increment_version(given)
     return o, lse
 
 

@@ -86,3 +86,40 @@ def test_workspace_in_pieces_is_refused(library):
     assert not library.calls
     decode(cache(), workspace=gpu(64, 128, dtype=torch.uint8))
     assert library.calls[0][1][-2] == 8192
+
+
+def test_writes_in_place_are_told_to_autograd(library):
+    """A graph that saved what a call writes over raises, as behind torch's own operations, and nothing else does."""
+    leaf = gpu(B, KV, 8, D).requires_grad_()
+    places = gpu(8, 2, dtype=torch.int32)
+
+    def saved():
+        x = leaf * 2
+        return x, (x * x).sum()
+
+    x, y = saved()
+    with torch.no_grad():
+        sa.rotary(x, None, places, (32, 32), out=(x, None))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    (q, y), (k, z) = saved(), saved()
+    with torch.no_grad():
+        sa.rotary(q, k, places, (32, 32), out=(gpu(B, KV, 8, D), k))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.backward()
+    y.backward()  # q was read alone
+    c = cache()
+    before = [t._version for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    x = gpu(B, KV, 5, D)
+    sa.store8(c, x, x)
+    assert all(t._version > old for t, old in zip((c.k, c.v, c.k_scale, c.v_scale), before)) and x._version == 0
+    q, out, lse = gpu(B, KV, D), gpu(B, KV, D), gpu(B, KV, dtype=torch.float32)
+    before = [t._version for t in (c.k, c.v, c.k_scale, c.v_scale)]
+    decode(c, q=q, out=out, lse=lse)
+    assert out._version > 0 and lse._version > 0 and q._version == 0
+    assert [t._version for t in (c.k, c.v, c.k_scale, c.v_scale)] == before
+    with torch.inference_mode():  # where tensors have no version
+        x = gpu(B, KV, 5, D)
+        sa.rotary(x, None, gpu(5, 1, dtype=torch.int32), (64,), out=(x, None))
+        sa.store8(cache(), x, x)
+        decode(cache(), out=gpu(B, KV, D), lse=gpu(B, KV, dtype=torch.float32))
