@@ -536,6 +536,8 @@ def _rotary_run(args, q, k, positions, inverse, out, stream):
                 if t is not None and (y.shape != t.shape or y.dtype != t.dtype or y.device != device
                                       or y.stride(-1) != 1):
                     raise ValueError("out must match q and k in shape, type and device, d contiguous")
+            if k is not None and (q_out.data_ptr() in (k.data_ptr(), k_out.data_ptr()) or k_out.data_ptr() == q.data_ptr()):
+                raise ValueError("out must be the inputs, each its own, or memory apart from them and from each other")
         # (the library itself, as in store8 and decode8: the entry points above would look at every argument again)
         st = lib().sparse_attn_rotary(
             *front, q.data_ptr(), _row_strides(shape, q_st), q_out.data_ptr(), _row_strides(shape, q_out.stride()),
@@ -554,8 +556,8 @@ def rotary(q, k, positions, axis_dims, base=10000.0, pairing=SA_ROTARY_ADJACENT,
     q [b, h, n, d] and k [b, kv_h, n, d] (k may be None), or [b, h, d] and [b, kv_h, d]
     for one token a sequence.  ``positions``: int32 [n, axes] or [b, n, axes] (one
     token: [b, axes]); ``axis_dims``: the elements of d that each axis owns.
-    ``inverse`` turns back, which is also the gradient.  ``out``: (q_out, k_out), the
-    inputs themselves allowed."""
+    ``inverse`` turns back, which is also the gradient.  ``out``: (q_out, k_out), each its
+    own input or memory apart from both inputs.  The result is not differentiable: ``Rotary``'s is."""
     return _rotary_run(_rotary_args(q, k, axis_dims, base, pairing), q, k, positions, inverse, out, stream)
 
 

@@ -123,3 +123,20 @@ def test_writes_in_place_are_told_to_autograd(library):
         sa.rotary(x, None, gpu(5, 1, dtype=torch.int32), (64,), out=(x, None))
         sa.store8(cache(), x, x)
         decode(cache(), out=gpu(B, KV, D), lse=gpu(B, KV, dtype=torch.float32))
+
+
+def test_rotary_outputs_over_each_other_are_refused(library):
+    """Workgroups turn q and k at once, in any order: an output may be its own input, not the other's, nor may both be one."""
+    q, k, places = gpu(B, KV, 8, D), gpu(B, KV, 8, D), gpu(8, 1, dtype=torch.int32)
+    other = gpu(B, KV, 8, D)
+    for out in ((k, q), (k, other), (other, q), (other, other), (q, q)):
+        with pytest.raises(ValueError, match="out"):
+            sa.rotary(q, k, places, (64,), out=out)
+    with pytest.raises(ValueError, match="out"):
+        sa.rotary(q, q, places, (64,), out=(q, q))
+    assert not library.calls
+    for out in ((q, k), (other, k), (q, other)):
+        sa.rotary(q, k, places, (64,), out=out)
+    sa.rotary(q, q, places, (64,), out=(other, k))  # read alone
+    sa.rotary(q, None, places, (64,), out=(q, None))
+    assert len(library.calls) == 5
