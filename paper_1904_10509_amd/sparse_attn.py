@@ -476,6 +476,11 @@ def _row_strides(shape, st):
                   st[2] if len(shape) == 4 and shape[2] > 1 else shape[-1])
 
 
+def _one_layout(shape, st, other):
+    """Whether the entry points would step over both alike."""
+    return st == other or st[-1] == other[-1] and tuple(_row_strides(shape, st)) == tuple(_row_strides(shape, other))
+
+
 def _check_ints(name, t, count, device):
     """A contiguous int32 tensor of `count` elements on the device."""
     if t.dtype != torch.int32 or t.shape != (count,) or not t.is_contiguous():
@@ -621,7 +626,7 @@ class Cache8:
         # (other types of eight bits have other values for the codes)
         if k.dtype not in _CODE_TYPES or v.dtype not in _CODE_TYPES:
             raise ValueError("the cache's k and v must be float8_e4m3fn or uint8 tensors")
-        if len(shape) != 4 or v.shape != shape or v.stride() != st:
+        if len(shape) != 4 or v.shape != shape or not _one_layout(shape, st, v.stride()):
             raise ValueError("the cache's k and v must be [batch, kv_heads, capacity, d] tensors of one layout")
         if shape[3] != d or st[3] != 1:
             raise ValueError("the cache must have the d of the tensors, contiguous")
@@ -646,12 +651,13 @@ def build_cache8(batch, kv_heads, capacity, d, block=64, device="cuda"):
 
 def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
     """Write new keys and values [b, kv_heads, n_new, d] (or [b, kv_heads, d]: one token) into the cache, the first
-    counts[b] of sequence b at positions start[b], ... (int32 [b] on the device; None: 0, and all of them)."""
+    counts[b] of sequence b at positions start[b], ... (int32 [b] on the device; None: 0, and all of them).  The library
+    takes one set of strides for k and v; where theirs differ, what is not contiguous is copied first."""
     shape, st, device, dtype = k.shape, k.stride(), k.device, k.dtype
-    if len(shape) not in (3, 4) or v.shape != shape or v.stride() != st or v.dtype != dtype or v.device != device:
-        raise ValueError("k and v must be [batch, kv_heads, n_new, d] (or [batch, kv_heads, d]) of one layout, type and "
-                         "GPU")
-    if device.type != "cuda" or dtype not in _DTYPE_CODES or st[-1] != 1:
+    v_st = v.stride()
+    if len(shape) not in (3, 4) or v.shape != shape or v.dtype != dtype or v.device != device:
+        raise ValueError("k and v must be [batch, kv_heads, n_new, d] (or [batch, kv_heads, d]) of one type and GPU")
+    if device.type != "cuda" or dtype not in _DTYPE_CODES or st[-1] != 1 or v_st[-1] != 1:
         raise ValueError("k and v must be bfloat16 or float32 on the GPU, d contiguous")
     b, h, d = shape[0], shape[1], shape[-1]
     cb, ch, capacity, cache_strides = cache._args(d, device)
@@ -662,6 +668,9 @@ def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
     if counts is not None:
         _check_ints("counts", counts, b, device)
     with _here(device, stream):
+        if not _one_layout(shape, st, v_st):
+            k, v = k.contiguous(), v.contiguous()
+            st = k.stride()
         st = lib().sparse_attn_cache8_store(
             b, h, shape[2] if len(shape) == 4 else 1, d, _DTYPE_CODES[dtype], k.data_ptr(), v.data_ptr(),
             _row_strides(shape, st), None if start is None else start.data_ptr(),

@@ -140,3 +140,39 @@ def test_rotary_outputs_over_each_other_are_refused(library):
     sa.rotary(q, q, places, (64,), out=(other, k))  # read alone
     sa.rotary(q, None, places, (64,), out=(q, None))
     assert len(library.calls) == 5
+
+
+def handed_over(call):
+    """Of a recorded store: the strides that the library steps over, and the addresses of k and v."""
+    return tuple(call[1][7]), call[1][5], call[1][6]
+
+
+def test_store_of_rotated_keys_and_values_from_a_projection(library):
+    """k comes out of rotary packed, v is a slice of the projection: where the strides that are stepped over are one set
+    neither is copied, else both reach the library packed.  The same for one token a sequence."""
+    c = cache()
+    for n in (7, 1):
+        qkv = torch.randn(B, n, 3, KV, D).to(torch.bfloat16).as_subclass(OnGpu)
+        k, v = (qkv[:, :, i].transpose(1, 2) for i in (1, 2))
+        sa.store8(c, k, v)  # of one layout: in place
+        assert handed_over(library.calls[-1])[1:] == (k.data_ptr(), v.data_ptr())
+        packed = k.contiguous()
+        sa.store8(c, packed, v)
+        strides, at_k, at_v = handed_over(library.calls[-1])
+        assert strides == (KV * n * D, n * D, D) and at_k == packed.data_ptr() and at_v != v.data_ptr()
+        if n == 1:
+            sa.store8(c, packed[:, :, 0], v[:, :, 0])
+            strides, at_k, at_v = handed_over(library.calls[-1])
+            assert strides == (KV * D, D, D) and at_k == packed.data_ptr()
+    # a dimension of one element is not stepped over: its stride does not tell layouts apart
+    one = cache()
+    one = sa.Cache8(one.k[:1], one.v[:1], one.k_scale[:1], one.v_scale[:1], T)
+    row = torch.randn(1, KV, 1, D).to(torch.bfloat16)
+    k, v = row.as_subclass(OnGpu), row.as_strided(row.shape, (7 * D, D, 9 * D, 1)).as_subclass(OnGpu)
+    assert k.stride() != v.stride()
+    sa.store8(one, k, v)
+    assert handed_over(library.calls[-1]) == ((0, D, D), k.data_ptr(), v.data_ptr())
+    with pytest.raises(ValueError):
+        sa.store8(c, gpu(B, KV, 5, D), gpu(B, KV, 6, D))
+    with pytest.raises(ValueError):
+        sa.store8(c, gpu(B, KV, 5, D), gpu(B, KV, 5, 2 * D)[..., ::2])
