@@ -544,10 +544,12 @@ def _rotary_run(args, q, k, positions, inverse, out, stream):
             if k is not None and (q_out.data_ptr() in (k.data_ptr(), k_out.data_ptr()) or k_out.data_ptr() == q.data_ptr()):
                 raise ValueError("out must be the inputs, each its own, or memory apart from them and from each other")
         # (the library itself, as in store8 and decode8: the entry points above would look at every argument again)
+        q_rows, k_rows = _row_strides(shape, q_st), _row_strides(k_shape, k_st)
+        qo_st, ko_st = q_out.stride(), k_st if k is None else k_out.stride()
         st = lib().sparse_attn_rotary(
-            *front, q.data_ptr(), _row_strides(shape, q_st), q_out.data_ptr(), _row_strides(shape, q_out.stride()),
-            None if k is None else k.data_ptr(), _row_strides(k_shape, k_st), None if k is None else k_out.data_ptr(),
-            None if k is None else _row_strides(k_shape, k_out.stride()), *places, *behind, 1 if inverse else 0,
+            *front, q.data_ptr(), q_rows, q_out.data_ptr(), q_rows if qo_st == q_st else _row_strides(shape, qo_st),
+            None if k is None else k.data_ptr(), k_rows, None if k is None else k_out.data_ptr(),
+            k_rows if ko_st == k_st else _row_strides(k_shape, ko_st), *places, *behind, 1 if inverse else 0,
             _stream(stream, device))
     _check("sparse_attn_rotary", st)
     if out is not None:  # written behind torch's back: a graph that saved these has to know
