@@ -300,7 +300,6 @@ def sparse_attn_cache8_store(batch, kv_heads, n_new, d_head, dtype, k, v, kv_str
                                         _ptr(counts), capacity, scale_block, _ptr(k_cache), _ptr(v_cache),
                                         cache_strides, _ptr(k_scale), _ptr(v_scale), _stream(stream, k.device))
     _check("sparse_attn_cache8_store", st)
-    increment_version((cache.k, cache.v, cache.k_scale, cache.v_scale))
 
 
 def sparse_attn_decode8_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads, d_head,
@@ -679,6 +678,7 @@ def store8(cache: Cache8, k, v, start=None, counts=None, stream=None):
             None if counts is None else counts.data_ptr(), capacity, cache.block, cache.k.data_ptr(), cache.v.data_ptr(),
             cache_strides, cache.k_scale.data_ptr(), cache.v_scale.data_ptr(), _stream(stream, device))
     _check("sparse_attn_cache8_store", st)
+    # written behind torch's back: a graph that saved these has to know
     increment_version((cache.k, cache.v, cache.k_scale, cache.v_scale))
 
 

@@ -176,3 +176,19 @@ def test_store_of_rotated_keys_and_values_from_a_projection(library):
         sa.store8(c, gpu(B, KV, 5, D), gpu(B, KV, 6, D))
     with pytest.raises(ValueError):
         sa.store8(c, gpu(B, KV, 5, D), gpu(B, KV, 5, 2 * D)[..., ::2])
+
+
+def test_entry_points_marshal_alone(library):
+    """The functions named like the C entry points take tensors, addresses or None and hand them on."""
+    t = gpu(B, KV, 8, D)
+    strides, two = (ctypes.c_int64 * 3)(1, 2, 3), (ctypes.c_int64 * 2)(4, 5)
+    at = t.data_ptr()
+    sa.sparse_attn_rotary(B, 8, KV, 0, D, sa.SA_BF16, t, strides, t, strides, None, None, None, None, t, two, 1,
+                          (ctypes.c_int32 * 1)(D), 10000.0, 0, 0)
+    sa.sparse_attn_cache8_store(B, KV, 8, D, sa.SA_BF16, t, t, strides, None, t, CAP, T, t, t, strides, t, t)
+    sa.sparse_attn_decode8(t, 9, 16, 0, sa.SA_STRIDED, sa.SA_MODE_MERGED, B, KV, KV, D, sa.SA_BF16, t, two, t, t, strides, t, t,
+                           CAP, T, 0.125, t, two, t, t, 64)
+    assert [name for name, _ in library.calls] == ["sparse_attn_rotary", "sparse_attn_cache8_store", "sparse_attn_decode8"]
+    assert library.calls[0][1][6] == at and library.calls[0][1][10] is None
+    assert library.calls[1][1][5] == at and library.calls[1][1][8] is None
+    assert library.calls[2][1][0] == at
