@@ -420,6 +420,111 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
                         const int64_t* o_strides, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * A key / value cache in pages, for sequences whose lengths are not known beforehand.
+ *   k_pages, v_pages  [pages, kv_heads, page, d_head] of type dtype, element strides
+ *                     page_strides[0..2] (page, head, token) for both, d contiguous.  Keys and
+ *                     values may interleave (v_pages = k_pages + d_head, token stride 2 d_head: a
+ *                     token's key and value lie together, which gathered tokens gain from).
+ *   page              tokens of a page, in {16, 32, 64, 128, 256};  pages * page < 2^31
+ *   table             int32 [sequences, max_pages], rows table_stride apart: entry i of a
+ *                     sequence is the page that holds its positions i * page .. (i + 1) * page - 1
+ *   slot              page number * page + place inside the page, an int32
+ * Every base address 16-byte aligned (integers 4), strides multiples of 16 bytes, the token
+ * stride >= d_head, pages and heads apart.
+ *
+ * sparse_attn_page_tables does the bookkeeping of a batch on the device: sequence s holds
+ * held[s] tokens in the cache and brings fresh[s] new ones (one, when it generates), which lie
+ * packed behind those of the sequences before it.
+ *   table     in / out: the entries of the pages that the sequences need and do not hold yet
+ *             (ceil((held + fresh) / page) - ceil(held / page)) are filled in, sequence by sequence,
+ *             from the front of free_pages; no other entry is touched.  table_stride >= max_pages.
+ *   free_pages  device int32 [free_count]: pages that nobody holds (free_count = 0: may be NULL)
+ *   tokens    rows of the packed batch, >= 1; rows behind the last sequence are padding
+ *   starts    out, int32 [sequences + 1]: first row of every sequence, and the rows in use
+ *   positions out, int32 [tokens]: the row's position in its sequence
+ *   slots     out, int32 [tokens]: where sparse_attn_paged_store puts the row
+ *   last      out, int32 [sequences]: position of the sequence's last token (held + fresh - 1; -1 for
+ *             none), where a decoding step stands
+ *   taken     out, int32 [1]: pages that the call needed; the caller's list goes on behind them
+ * Negative lengths are taken as 0, a held length above max_pages * page as that.  Rows that have no
+ * place have position and slot -1 (padding, and tokens behind the table's last page) or slot -1 (the
+ * list was short: taken > free_count, and the table's entry is -1).  Rows beyond `tokens` do not
+ * count: starts ends there, and no pages are taken for them.  The outputs must not overlap.
+ * SA_ERR_UNSUPPORTED for more than 8,000 sequences or a table of 2^31 tokens or more a sequence.
+ */
+int sparse_attn_page_tables(int32_t sequences, const int32_t* held, const int32_t* fresh, int32_t page,
+                            int32_t max_pages, int32_t* table, int64_t table_stride, const int32_t* free_pages,
+                            int64_t free_count, int64_t tokens, int32_t* starts, int32_t* positions, int32_t* slots,
+                            int32_t* last, int32_t* taken, void* stream);
+
+/*
+ * New keys and values into the pages: row t of k and v, [tokens, kv_heads, d_head] of the cache's
+ * type with element strides k_strides[0..1], v_strides[0..1] (token, head) and d contiguous, goes to
+ * slots[t] (device int32 [tokens]).  A slot below 0 or outside the pool is not stored; two rows of
+ * one slot leave one of them, or parts of both, there.  Nothing else of the cache is touched.
+ */
+int sparse_attn_paged_store(int64_t tokens, int32_t kv_heads, int32_t d_head, int32_t dtype, const void* k,
+                            const int64_t* k_strides, const void* v, const int64_t* v_strides, const int32_t* slots,
+                            void* k_pages, void* v_pages, const int64_t* page_strides, int64_t pages, int32_t page,
+                            void* stream);
+
+/*
+ * sparse_attn_decode over a cache in pages, every sequence at a position of its own: as
+ * sparse_attn_decode8 (positions, max_pos, heads that share cache heads, o, lse, a negative
+ * position, one above max_pos), with keys and values of q's type found through the table.
+ *   table_stride  0: one row for the whole batch;  max_pos < max_pages * page
+ * Entries of the table that hold no attended position are not read; one that does and is no page of
+ * the pool makes the row's o and lse NaN.  q . k, the softmax and the sums are in fp32; bf16 weights
+ * enter the product with V with 16 bits.  A NaN or an infinity among a row's own keys and values
+ * makes what depends on it NaN or infinite; other rows of the cache are never read into a result.
+ * batch * heads < 2^22, else SA_ERR_UNSUPPORTED.
+ */
+int sparse_attn_paged_decode_workspace_size(int64_t max_pos, int32_t stride_l, int32_t summary_c, int32_t pattern,
+                                            int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                                            int32_t d_head, int32_t dtype, size_t* bytes);
+
+int sparse_attn_paged_decode(const int32_t* positions, int64_t max_pos, int32_t stride_l, int32_t summary_c,
+                             int32_t pattern, int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                             int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides,
+                             const void* k_pages, const void* v_pages, const int64_t* page_strides, int64_t pages,
+                             int32_t page, const int32_t* table, int64_t table_stride, int32_t max_pages,
+                             float softmax_scale, void* o, const int64_t* o_strides, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * sparse_attn_fwd over sequences of any lengths packed one behind the other (the prompts of a
+ * batch), without a layout and without a gradient: row i of a sequence attends S_i (Sec. 4.3, 5.1)
+ * within its own sequence.
+ *   starts   device int32 [sequences + 1], ascending: sequence s is rows starts[s] .. starts[s + 1] - 1
+ *            (none where both are equal).  Read when the call runs.  Rows outside all sequences keep
+ *            what o and lse hold; values outside 0 .. tokens are taken as the nearest of both.
+ *   tokens   rows of the tensors
+ *   heads, kv_heads  kv_heads divides heads; query head h reads key head h / (heads / kv_heads) and
+ *            attends the set of head h
+ *   q, o     [tokens, heads, d_head], k, v [tokens, kv_heads, d_head] of type dtype, element strides
+ *            [0..1] (token, head) of their own, d contiguous (q, k and v may be parts of one tensor);
+ *            o's rows must not overlap, nor lie in the inputs
+ *   lse      device output [heads, tokens] contiguous fp32: natural log, -inf (and o = 0) for an empty set
+ * Any length, also 1, and any stride: n is no multiple of anything.  l >= the longest sequence with
+ * SA_STRIDED, SA_MODE_A1 is dense causal attention.  Precision as sparse_attn_fwd (bf16 weights are
+ * rounded once for the product with V).  An infinity or a NaN reaches the rows that attend it alone.
+ * Addresses 16-byte aligned (starts and lse 4), strides multiples of 16 bytes.
+ * workspace: sparse_attn_packed_workspace_size bytes (0 but for strided merged heads with 2 l <
+ * tokens), 16-byte aligned, contents ignored; calls that share one must not overlap.
+ * SA_ERR_UNSUPPORTED for more than 2^20 sequences, 65,535 heads or 2^31 - 1,025 tokens.
+ */
+int sparse_attn_packed_workspace_size(int64_t tokens, int32_t stride_l, int32_t summary_c, int32_t pattern,
+                                      int32_t head_mode, int32_t heads, int32_t kv_heads, int32_t d_head,
+                                      int32_t dtype, size_t* bytes);
+
+int sparse_attn_packed_fwd(int32_t sequences, const int32_t* starts, int64_t tokens, int32_t stride_l,
+                           int32_t summary_c, int32_t pattern, int32_t head_mode, int32_t heads, int32_t kv_heads,
+                           int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides, const void* k,
+                           const int64_t* k_strides, const void* v, const int64_t* v_strides, float softmax_scale,
+                           void* o, const int64_t* o_strides, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
  * Strided pattern, merged heads (SA_STRIDED, SA_MODE_MERGED), with the A2
  * part computed by transposition (Sec. 5.5: reordered by residue mod l, a
  * stride of l becomes a local window), with the caller choosing the class

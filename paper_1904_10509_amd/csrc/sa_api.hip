@@ -344,6 +344,47 @@ int check_cache8(const void* k, const void* v, const int64_t* strides, const flo
     return SA_OK;
 }
 
+// Rows of a packed call: the kernels count keys past a tile's last one in 32 bits.
+constexpr int64_t kMaxPackedTokens = INT32_MAX - 1024;
+
+// Pattern and shape of a call on packed sequences.
+int check_packed(int64_t tokens, int32_t l, int32_t c, int32_t pattern, int32_t mode, int32_t heads, int32_t kv_heads,
+                 int32_t d, int32_t dtype, sa::PackedCall* p) {
+    int st = check_pattern_code(l, c, pattern, mode, &p->pattern, &p->sub);
+    if (st != SA_OK) return st;
+    st = check_decode_shape(1, heads, d, dtype);
+    if (st != SA_OK) return st;
+    if (tokens < 1 || kv_heads < 1 || heads % kv_heads != 0) return SA_ERR_INVALID;
+    if (tokens > kMaxPackedTokens || heads > 65535) return SA_ERR_UNSUPPORTED;
+    p->tokens = tokens;
+    p->mode = mode;
+    p->l = l;
+    p->c = c;
+    p->heads = heads;
+    p->kv_heads = kv_heads;
+    p->d = d;
+    p->dtype = dtype;
+    return SA_OK;
+}
+
+// A cache in pages and the shape of what it holds.
+int check_pages(const void* k, const void* v, const int64_t* strides, int64_t pages, int32_t page, int32_t kv_heads,
+                int32_t d, int32_t dtype, sa::PagedCache* out, int32_t* shift) {
+    if (pages < 1 || pages > INT32_MAX) return SA_ERR_INVALID;
+    if (page != 16 && page != 32 && page != 64 && page != 128 && page != 256) return SA_ERR_INVALID;
+    if (pages * page > INT32_MAX) return SA_ERR_UNSUPPORTED;  // a slot is an int32
+    if (!k || !v || !strides || !aligned16(k) || !aligned16(v)) return SA_ERR_INVALID;
+    const int64_t size = dtype == SA_BF16 ? 2 : 4;
+    if (!rows_ok(strides, 3, 16 / size, d) || !rows_apart(strides, (int32_t)pages, kv_heads, d)) return SA_ERR_INVALID;
+    out->k = (uint8_t*)const_cast<void*>(k);
+    out->v = (uint8_t*)const_cast<void*>(v);
+    out->sp = strides[0] * size;
+    out->sh = strides[1] * size;
+    out->st = strides[2] * size;
+    *shift = __builtin_ctz((unsigned)page);
+    return SA_OK;
+}
+
 // Merged strided heads by transposition through the explicit entry points:
 // the band over the caller's strided A1 layout, the classes in blocks of
 // class_block (see class_args); tensors contiguous.
@@ -803,6 +844,171 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
                               static_cast<hipStream_t>(stream)) == hipSuccess
                ? SA_OK
                : SA_ERR_HIP;
+}
+
+int sparse_attn_page_tables(int32_t sequences, const int32_t* held, const int32_t* fresh, int32_t page,
+                            int32_t max_pages, int32_t* table, int64_t table_stride, const int32_t* free_pages,
+                            int64_t free_count, int64_t tokens, int32_t* starts, int32_t* positions, int32_t* slots,
+                            int32_t* last, int32_t* taken, void* stream) {
+    if (sequences < 1 || tokens < 1 || tokens > kMaxPackedTokens || max_pages < 1) return SA_ERR_INVALID;
+    if (page != 16 && page != 32 && page != 64 && page != 128 && page != 256) return SA_ERR_INVALID;
+    if (free_count < 0 || free_count > INT32_MAX || (free_count > 0 && !free_pages)) return SA_ERR_INVALID;
+    if (table_stride < 0 || (sequences > 1 && table_stride < max_pages)) return SA_ERR_INVALID;
+    if (!held || !fresh || !table || !starts || !positions || !slots || !last || !taken) return SA_ERR_INVALID;
+    for (const void* p : {(const void*)held, (const void*)fresh, (const void*)table, (const void*)free_pages,
+                          (const void*)starts, (const void*)positions, (const void*)slots, (const void*)last,
+                          (const void*)taken})
+        if (!aligned4(p)) return SA_ERR_INVALID;
+    if (sequences > sa::kMaxTableSequences || (int64_t)max_pages * page > INT32_MAX) return SA_ERR_UNSUPPORTED;
+    sa::PageTables a;
+    a.sequences = sequences;
+    a.held = held;
+    a.fresh = fresh;
+    a.shift = __builtin_ctz((unsigned)page);
+    a.max_pages = max_pages;
+    a.table = table;
+    a.table_stride = table_stride;
+    a.free_pages = free_pages;
+    a.free_count = (int32_t)free_count;
+    a.tokens = tokens;
+    a.starts = starts;
+    a.positions = positions;
+    a.slots = slots;
+    a.last = last;
+    a.taken = taken;
+    a.wide = aligned16(positions) && aligned16(slots);
+    return sa::page_tables_launch(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sparse_attn_paged_store(int64_t tokens, int32_t kv_heads, int32_t d_head, int32_t dtype, const void* k,
+                            const int64_t* k_strides, const void* v, const int64_t* v_strides, const int32_t* slots,
+                            void* k_pages, void* v_pages, const int64_t* page_strides, int64_t pages, int32_t page,
+                            void* stream) {
+    int st = check_decode_shape(1, kv_heads, d_head, dtype);
+    if (st != SA_OK) return st;
+    if (tokens < 1 || tokens > kMaxPackedTokens) return SA_ERR_INVALID;
+    sa::PagedStore a;
+    st = check_pages(k_pages, v_pages, page_strides, pages, page, kv_heads, d_head, dtype, &a.cache, &a.shift);
+    if (st != SA_OK) return st;
+    if (!k || !v || !k_strides || !v_strides || !slots) return SA_ERR_INVALID;
+    if (!aligned16(k) || !aligned16(v) || !aligned4(slots)) return SA_ERR_INVALID;
+    const int64_t size = dtype == SA_BF16 ? 2 : 4;
+    if (!rows_ok(k_strides, 2, 16 / size, 0) || !rows_ok(v_strides, 2, 16 / size, 0)) return SA_ERR_INVALID;
+    if (kv_heads > 65535) return SA_ERR_UNSUPPORTED;
+    a.tokens = tokens;
+    a.heads = kv_heads;
+    a.pages = (int32_t)pages;
+    a.piece_shift = __builtin_ctz((unsigned)(d_head * size / 16));
+    a.k = static_cast<const uint8_t*>(k);
+    a.v = static_cast<const uint8_t*>(v);
+    a.kt = k_strides[0] * size;
+    a.kh = k_strides[1] * size;
+    a.vt = v_strides[0] * size;
+    a.vh = v_strides[1] * size;
+    a.slots = slots;
+    return sa::paged_store_launch(a, static_cast<hipStream_t>(stream)) == hipSuccess ? SA_OK : SA_ERR_HIP;
+}
+
+int sparse_attn_paged_decode_workspace_size(int64_t max_pos, int32_t stride_l, int32_t summary_c, int32_t pattern,
+                                            int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                                            int32_t d_head, int32_t dtype, size_t* bytes) {
+    int32_t internal = 0, sub = 0;
+    int st = check_decode_pattern(max_pos, stride_l, summary_c, pattern, head_mode, &internal, &sub);
+    if (st != SA_OK) return st;
+    st = check_decode_shape(batch, heads, d_head, dtype);
+    if (st != SA_OK) return st;
+    if (kv_heads < 1 || heads % kv_heads != 0 || !bytes) return SA_ERR_INVALID;
+    if ((int64_t)batch * heads >= kMaxRows8) return SA_ERR_UNSUPPORTED;
+    *bytes = sa::paged_decode_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c, batch,
+                                              heads, kv_heads, d_head, dtype);
+    return SA_OK;
+}
+
+int sparse_attn_paged_decode(const int32_t* positions, int64_t max_pos, int32_t stride_l, int32_t summary_c,
+                             int32_t pattern, int32_t head_mode, int32_t batch, int32_t heads, int32_t kv_heads,
+                             int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides,
+                             const void* k_pages, const void* v_pages, const int64_t* page_strides, int64_t pages,
+                             int32_t page, const int32_t* table, int64_t table_stride, int32_t max_pages,
+                             float softmax_scale, void* o, const int64_t* o_strides, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    int32_t internal = 0, sub = 0;
+    int st = check_decode_pattern(max_pos, stride_l, summary_c, pattern, head_mode, &internal, &sub);
+    if (st != SA_OK) return st;
+    st = check_decode_shape(batch, heads, d_head, dtype);
+    if (st != SA_OK) return st;
+    if (kv_heads < 1 || heads % kv_heads != 0) return SA_ERR_INVALID;
+    if ((int64_t)batch * heads >= kMaxRows8) return SA_ERR_UNSUPPORTED;
+    sa::PagedStep p;
+    st = check_pages(k_pages, v_pages, page_strides, pages, page, kv_heads, d_head, dtype, &p.cache, &p.shift);
+    if (st != SA_OK) return st;
+    if (max_pages < 1 || max_pos >= (int64_t)max_pages * page) return SA_ERR_INVALID;
+    if (table_stride < 0 || (batch > 1 && table_stride != 0 && table_stride < max_pages)) return SA_ERR_INVALID;
+    if (!positions || !q || !q_strides || !table || !o || !o_strides || !lse) return SA_ERR_INVALID;
+    if (!aligned4(positions) || !aligned4(table) || !aligned16(q) || !aligned16(o) || !aligned4(lse)) return SA_ERR_INVALID;
+    const int64_t unit = dtype == SA_BF16 ? 8 : 4;  // elements per 16 bytes
+    if (!rows_ok(q_strides, 2, unit, 0) || !rows_ok(o_strides, 2, unit, 0)) return SA_ERR_INVALID;
+    if (!rows_apart(o_strides, batch, heads, d_head)) return SA_ERR_INVALID;
+    if (!isfinite(softmax_scale) || !(softmax_scale > 0.f)) return SA_ERR_INVALID;
+    const size_t need = sa::paged_decode_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c,
+                                                         batch, heads, kv_heads, d_head, dtype);
+    if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
+    if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
+    p.table = table;
+    p.positions = positions;
+    p.table_stride = table_stride;
+    p.pages = (int32_t)pages;
+    return sa::paged_decode_launch(p, internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c, batch, heads,
+                                   kv_heads, d_head, dtype, q, q_strides, softmax_scale, o, o_strides, lse, workspace,
+                                   static_cast<hipStream_t>(stream)) == hipSuccess
+               ? SA_OK
+               : SA_ERR_HIP;
+}
+
+int sparse_attn_packed_workspace_size(int64_t tokens, int32_t stride_l, int32_t summary_c, int32_t pattern,
+                                      int32_t head_mode, int32_t heads, int32_t kv_heads, int32_t d_head,
+                                      int32_t dtype, size_t* bytes) {
+    sa::PackedCall p;
+    const int st = check_packed(tokens, stride_l, summary_c, pattern, head_mode, heads, kv_heads, d_head, dtype, &p);
+    if (st != SA_OK) return st;
+    if (!bytes) return SA_ERR_INVALID;
+    *bytes = sa::packed_workspace_bytes(tokens, p.pattern, head_mode, stride_l, heads, d_head);
+    return SA_OK;
+}
+
+int sparse_attn_packed_fwd(int32_t sequences, const int32_t* starts, int64_t tokens, int32_t stride_l,
+                           int32_t summary_c, int32_t pattern, int32_t head_mode, int32_t heads, int32_t kv_heads,
+                           int32_t d_head, int32_t dtype, const void* q, const int64_t* q_strides, const void* k,
+                           const int64_t* k_strides, const void* v, const int64_t* v_strides, float softmax_scale,
+                           void* o, const int64_t* o_strides, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+    sa::PackedCall p;
+    const int st = check_packed(tokens, stride_l, summary_c, pattern, head_mode, heads, kv_heads, d_head, dtype, &p);
+    if (st != SA_OK) return st;
+    if (sequences < 1) return SA_ERR_INVALID;
+    if (sequences > (1 << 20)) return SA_ERR_UNSUPPORTED;
+    if (!starts || !q || !q_strides || !k || !k_strides || !v || !v_strides || !o || !o_strides || !lse)
+        return SA_ERR_INVALID;
+    if (!aligned4(starts) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned4(lse))
+        return SA_ERR_INVALID;
+    const int64_t unit = dtype == SA_BF16 ? 8 : 4;  // elements per 16 bytes
+    for (const int64_t* strides : {q_strides, k_strides, v_strides, o_strides})
+        if (!rows_ok(strides, 2, unit, 0)) return SA_ERR_INVALID;
+    if (!rows_apart(o_strides, tokens > 1 ? 2 : 1, heads, d_head)) return SA_ERR_INVALID;
+    if (!isfinite(softmax_scale) || !(softmax_scale > 0.f)) return SA_ERR_INVALID;
+    const size_t need = sa::packed_workspace_bytes(tokens, p.pattern, head_mode, stride_l, heads, d_head);
+    if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
+    if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
+    p.starts = starts;
+    p.sequences = sequences;
+    p.q = q, p.k = k, p.v = v, p.o = o;
+    p.qt = q_strides[0], p.qh = q_strides[1];
+    p.kt = k_strides[0], p.kh = k_strides[1];
+    p.vt = v_strides[0], p.vh = v_strides[1];
+    p.ot = o_strides[0], p.oh = o_strides[1];
+    p.scale = softmax_scale;
+    p.lse = lse;
+    p.workspace = static_cast<float*>(workspace);
+    return sa::packed_launch(p, static_cast<hipStream_t>(stream)) == hipSuccess ? SA_OK : SA_ERR_HIP;
 }
 
 int sparse_attn_transposed_workspace_size(int64_t n, int32_t block, int32_t stride_l, int32_t class_block,

@@ -356,6 +356,67 @@ hipError_t decode8_launch(const Cache8& cache, const int32_t* positions, int pat
                           const void* q, const int64_t* q_strides, float scale, void* o, const int64_t* o_strides,
                           float* lse, void* workspace, hipStream_t stream);
 
+// A key / value cache in pages (sa_paged.hip, sa_paged_decode.hip): [pages, kv_heads, page, d].
+struct PagedCache {
+    uint8_t *k, *v;
+    int64_t sp, sh, st;           // byte strides: page, head, token
+};
+// Page tables, first rows, positions and slots of a batch, from the sequences' lengths.
+struct PageTables {
+    int32_t sequences;
+    const int32_t *held, *fresh;
+    int32_t shift;                // log2 of a page's tokens
+    int32_t max_pages;
+    int32_t* table;
+    int64_t table_stride;
+    const int32_t* free_pages;
+    int32_t free_count;
+    int64_t tokens;
+    int32_t *starts, *positions, *slots, *last, *taken;
+    bool wide;                    // positions and slots in whole 16 bytes
+};
+constexpr int32_t kMaxTableSequences = 8000;  // two sums of each in LDS
+hipError_t page_tables_launch(const PageTables& a, hipStream_t stream);
+struct PagedStore {
+    PagedCache cache;
+    int64_t tokens;
+    int32_t heads, pages, shift;
+    int32_t piece_shift;          // log2 of the 16-byte pieces of a row
+    const uint8_t *k, *v;
+    int64_t kt, kh, vt, vh;       // byte strides: token, head
+    const int32_t* slots;
+};
+hipError_t paged_store_launch(const PagedStore& a, hipStream_t stream);
+struct PagedStep {
+    PagedCache cache;
+    const int32_t *table, *positions;
+    int64_t table_stride;
+    int32_t pages, shift;
+};
+size_t paged_decode_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c,
+                                    int batch, int heads, int kv_heads, int d, int dtype);
+hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l,
+                               int32_t c, int batch, int heads, int kv_heads, int d, int dtype, const void* q,
+                               const int64_t* q_strides, float scale, void* o, const int64_t* o_strides, float* lse,
+                               void* workspace, hipStream_t stream);
+
+// Attention over prompts packed one behind the other (sa_packed.hip).
+struct PackedCall {
+    const int32_t* starts;
+    int32_t sequences;
+    int64_t tokens;
+    int32_t pattern, mode, sub, l, c;
+    int32_t heads, kv_heads, d, dtype;
+    const void *q, *k, *v;
+    void* o;
+    int64_t qt, qh, kt, kh, vt, vh, ot, oh;  // element strides: token, head
+    float scale;
+    float* lse;                   // [heads, tokens]
+    float* workspace;
+};
+size_t packed_workspace_bytes(int64_t tokens, int32_t pattern, int32_t mode, int32_t l, int32_t heads, int32_t d);
+hipError_t packed_launch(const PackedCall& c, hipStream_t stream);
+
 size_t bwd_workspace_bytes(int64_t batch, int64_t heads, int64_t n, int64_t nq, int n_layouts);
 
 // Launches of a backward call: the row statistics (pre), dQ, and dK / dV.

@@ -86,6 +86,12 @@ __device__ inline void dma_b32(const void* sbase, uint32_t voff, uint32_t lds_wi
                  : : "v"(voff), "s"(sbase), "s"(lds_window) : "memory");
 }
 
+// The same from an address of each lane's own, for rows that lie anywhere.
+__device__ inline void dma_b128_at(const void* p, uint32_t lds_window) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off"
+                 : : "v"(p), "s"(lds_window) : "memory");
+}
+
 // Issues the direct-to-LDS loads of one BLK x D tile (rows 0..BLK-1 at row
 // stride ss elements) spread over NW waves.  Each lane's byte offsets inside
 // the tile are the same for every tile and computed once.

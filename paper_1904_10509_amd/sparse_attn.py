@@ -44,6 +44,12 @@ EXPORTED = (
     "sparse_attn_cache8_store",
     "sparse_attn_decode8_workspace_size",
     "sparse_attn_decode8",
+    "sparse_attn_page_tables",
+    "sparse_attn_paged_store",
+    "sparse_attn_paged_decode_workspace_size",
+    "sparse_attn_paged_decode",
+    "sparse_attn_packed_workspace_size",
+    "sparse_attn_packed_fwd",
     "sparse_attn_transposed_workspace_size",
     "sparse_attn_fwd_transposed",
     "sparse_attn_bwd_transposed",
@@ -87,6 +93,14 @@ def lib():
         L.sparse_attn_decode8_workspace_size.argtypes = _DEC + [_i32] * 5 + [_vp]
         L.sparse_attn_decode8.argtypes = ([_vp] + _DEC + [_i32] * 5 + [_vp] * 7 + [_i64, _i32, _f32] + [_vp] * 4
                                           + [_sz, _vp])
+        L.sparse_attn_page_tables.argtypes = ([_i32, _vp, _vp, _i32, _i32, _vp, _i64, _vp, _i64, _i64] + [_vp] * 6)
+        L.sparse_attn_paged_store.argtypes = [_i64] + [_i32] * 3 + [_vp] * 8 + [_i64, _i32, _vp]
+        L.sparse_attn_paged_decode_workspace_size.argtypes = _DEC + [_i32] * 5 + [_vp]
+        L.sparse_attn_paged_decode.argtypes = ([_vp] + _DEC + [_i32] * 5 + [_vp] * 5 + [_i64, _i32, _vp, _i64, _i32, _f32]
+                                               + [_vp] * 4 + [_sz, _vp])
+        _PAC = [_i64] + [_i32] * 8  # tokens, stride_l, summary_c, pattern, head_mode, heads, kv_heads, d_head, dtype
+        L.sparse_attn_packed_workspace_size.argtypes = _PAC + [_vp]
+        L.sparse_attn_packed_fwd.argtypes = [_i32, _vp] + _PAC + [_vp] * 6 + [_f32] + [_vp] * 4 + [_sz, _vp]
         _TR = [_i64, _i32, _i32, _i32]  # n, block, stride_l, class_block
         L.sparse_attn_transposed_workspace_size.argtypes = _TR + [_i32] * 4 + [_vp]
         L.sparse_attn_fwd_transposed.argtypes = _TR + [_vp] * 3 + [_i32] * 4 + [_vp] * 3 + [_f32] + [_vp] * 3 + [_sz, _vp]
@@ -320,6 +334,60 @@ def sparse_attn_decode8(positions, max_pos, stride_l, summary_c, pattern, head_m
                                    _ptr(o), o_strides, _ptr(lse), _ptr(workspace), workspace_bytes,
                                    _stream(stream, q.device))
     _check("sparse_attn_decode8", st)
+
+
+def sparse_attn_page_tables(sequences, held, fresh, page, max_pages, table, table_stride, free_pages, free_count, tokens,
+                            starts, positions, slots, last, taken, stream=None):
+    st = lib().sparse_attn_page_tables(sequences, _ptr(held), _ptr(fresh), page, max_pages, _ptr(table), table_stride,
+                                       _ptr(free_pages), free_count, tokens, _ptr(starts), _ptr(positions), _ptr(slots),
+                                       _ptr(last), _ptr(taken), _stream(stream, table.device))
+    _check("sparse_attn_page_tables", st)
+
+
+def sparse_attn_paged_store(tokens, kv_heads, d_head, dtype, k, k_strides, v, v_strides, slots, k_pages, v_pages,
+                            page_strides, pages, page, stream=None):
+    st = lib().sparse_attn_paged_store(tokens, kv_heads, d_head, dtype, _ptr(k), k_strides, _ptr(v), v_strides,
+                                       _ptr(slots), _ptr(k_pages), _ptr(v_pages), page_strides, pages, page,
+                                       _stream(stream, k.device))
+    _check("sparse_attn_paged_store", st)
+
+
+def sparse_attn_paged_decode_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads,
+                                            d_head, dtype):
+    out = ctypes.c_size_t(0)
+    st = lib().sparse_attn_paged_decode_workspace_size(max_pos, stride_l, summary_c, pattern, head_mode, batch, heads,
+                                                       kv_heads, d_head, dtype, ctypes.byref(out))
+    _check("sparse_attn_paged_decode_workspace_size", st)
+    return out.value
+
+
+def sparse_attn_paged_decode(positions, max_pos, stride_l, summary_c, pattern, head_mode, batch, heads, kv_heads, d_head,
+                             dtype, q, q_strides, k_pages, v_pages, page_strides, pages, page, table, table_stride,
+                             max_pages, softmax_scale, o, o_strides, lse, workspace, workspace_bytes, stream=None):
+    st = lib().sparse_attn_paged_decode(_ptr(positions), max_pos, stride_l, summary_c, pattern, head_mode, batch, heads,
+                                        kv_heads, d_head, dtype, _ptr(q), q_strides, _ptr(k_pages), _ptr(v_pages),
+                                        page_strides, pages, page, _ptr(table), table_stride, max_pages, softmax_scale,
+                                        _ptr(o), o_strides, _ptr(lse), _ptr(workspace), workspace_bytes,
+                                        _stream(stream, q.device))
+    _check("sparse_attn_paged_decode", st)
+
+
+def sparse_attn_packed_workspace_size(tokens, stride_l, summary_c, pattern, head_mode, heads, kv_heads, d_head, dtype):
+    out = ctypes.c_size_t(0)
+    st = lib().sparse_attn_packed_workspace_size(tokens, stride_l, summary_c, pattern, head_mode, heads, kv_heads, d_head,
+                                                 dtype, ctypes.byref(out))
+    _check("sparse_attn_packed_workspace_size", st)
+    return out.value
+
+
+def sparse_attn_packed_fwd(sequences, starts, tokens, stride_l, summary_c, pattern, head_mode, heads, kv_heads, d_head,
+                           dtype, q, q_strides, k, k_strides, v, v_strides, softmax_scale, o, o_strides, lse, workspace,
+                           workspace_bytes, stream=None):
+    st = lib().sparse_attn_packed_fwd(sequences, _ptr(starts), tokens, stride_l, summary_c, pattern, head_mode, heads,
+                                      kv_heads, d_head, dtype, _ptr(q), q_strides, _ptr(k), k_strides, _ptr(v), v_strides,
+                                      softmax_scale, _ptr(o), o_strides, _ptr(lse), _ptr(workspace), workspace_bytes,
+                                      _stream(stream, q.device))
+    _check("sparse_attn_packed_fwd", st)
 
 
 # ---------------------------------------------------------------------------
@@ -728,6 +796,231 @@ def decode8(q, cache: Cache8, positions, stride_l, summary_c, pattern, head_mode
             _I64x2(o_st[0] if b > 1 else 0, o_st[1] if h > 1 else 0), lse.data_ptr(), workspace.data_ptr(), need,
             _stream(stream, device))
     _check("sparse_attn_decode8", status)
+    if given:
+        increment_version(given)
+    return o, lse
+
+
+# ---------------------------------------------------------------------------
+# Sequences of any lengths: packed prompts, a cache in pages, and decoding over it
+# ---------------------------------------------------------------------------
+@dataclass
+class PagedCache:
+    """Keys and values in pages: k, v [pages, kv_heads, page, d] in bfloat16 or float32, with one set of strides."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    def _args(self, d, device, dtype):
+        """Pages, heads, tokens of a page and strides, checked."""
+        k, v = self.k, self.v
+        shape, st = k.shape, k.stride()
+        if len(shape) != 4 or v.shape != shape or not _one_layout(shape, st, v.stride()):
+            raise ValueError("the cache's k and v must be [pages, kv_heads, page, d] tensors of one layout")
+        if k.dtype != dtype or v.dtype != dtype:
+            raise ValueError("the cache must have the type of the other tensors")
+        if shape[3] != d or st[3] != 1:
+            raise ValueError("the cache must have the d of the tensors, contiguous")
+        if k.device != device or v.device != device:
+            raise ValueError("the cache must be on the device of the other tensors")
+        return shape[0], shape[1], shape[2], _row_strides(shape, st)
+
+
+def build_paged_cache(pages, kv_heads, page, d, dtype=torch.bfloat16, device="cuda"):
+    """An empty cache of pages.  A token's key and value lie side by side: the patterns that gather single tokens read
+    them in one piece."""
+    kv = torch.empty((pages, kv_heads, page, 2, d), dtype=dtype, device=device)
+    return PagedCache(kv[..., 0, :], kv[..., 1, :])
+
+
+@dataclass
+class PageMap:
+    """What ``page_tables`` makes of a batch's lengths, int32 on the device: starts [sequences + 1], positions [tokens],
+    slots [tokens], last [sequences] and taken [1]."""
+    starts: torch.Tensor
+    positions: torch.Tensor
+    slots: torch.Tensor
+    last: torch.Tensor
+    taken: torch.Tensor
+
+
+def _check_table(table, device):
+    """Sequences, entries and stride of a page table."""
+    shape = table.shape
+    if len(shape) != 2 or table.dtype != torch.int32 or table.device != device:
+        raise ValueError("table must be an int32 [sequences, max_pages] tensor on the device of the other tensors")
+    st = table.stride()
+    if shape[1] > 1 and st[1] != 1:
+        raise ValueError("table must have the entries of a sequence contiguous")
+    return shape[0], shape[1], st[0] if shape[0] > 1 else shape[1]
+
+
+def page_tables(table, held, fresh, free, page, tokens, out=None, stream=None):
+    """The bookkeeping of a batch of sequences that hold ``held`` tokens in the cache and bring ``fresh`` ones (int32
+    [sequences] on the device), packed into ``tokens`` rows: fills the new pages' entries of ``table`` (int32
+    [sequences, max_pages], in place) from the front of the list ``free`` (int32), and returns a ``PageMap``.  ``out``: a
+    ``PageMap`` to write into."""
+    device = table.device
+    if device.type != "cuda":
+        raise ValueError("table must be on the GPU")
+    sequences, max_pages, stride = _check_table(table, device)
+    _check_ints("held", held, sequences, device)
+    _check_ints("fresh", fresh, sequences, device)
+    if free.dim() != 1:
+        raise ValueError("free must have one dimension")
+    _check_ints("free", free, free.shape[0], device)
+    with _here(device, stream):
+        if out is None:
+            # one allocation; slots and positions in whole 16 bytes
+            rows = max(0, tokens + 3) // 4 * 4
+            x = table.new_empty(2 * rows + 2 * sequences + 2)
+            m = PageMap(x[2 * rows:2 * rows + sequences + 1], x[:max(0, tokens)], x[rows:rows + max(0, tokens)],
+                        x[2 * rows + sequences + 1:2 * rows + 2 * sequences + 1], x[2 * rows + 2 * sequences + 1:])
+        else:
+            m = out
+            for name, t, n in (("starts", m.starts, sequences + 1), ("positions", m.positions, tokens),
+                               ("slots", m.slots, tokens), ("last", m.last, sequences), ("taken", m.taken, 1)):
+                _check_ints(name, t, n, device)
+        st = lib().sparse_attn_page_tables(
+            sequences, held.data_ptr(), fresh.data_ptr(), page, max_pages, table.data_ptr(), stride, free.data_ptr(),
+            free.shape[0], tokens, m.starts.data_ptr(), m.positions.data_ptr(), m.slots.data_ptr(), m.last.data_ptr(),
+            m.taken.data_ptr(), _stream(stream, device))
+    _check("sparse_attn_page_tables", st)
+    # written behind torch's back: a graph that saved these has to know
+    increment_version((table,) if out is None else (table, m.starts, m.positions, m.slots, m.last, m.taken))
+    return m
+
+
+def _token_strides(shape, st):
+    """Strides (token, head) of a [tokens, heads, d] tensor as the entry points take them (see _row_strides)."""
+    return _I64x2(st[0] if shape[0] > 1 else shape[1] * shape[2] * 2, st[1] if shape[1] > 1 else shape[2])
+
+
+def paged_store(cache: PagedCache, k, v, slots, stream=None):
+    """Write new keys and values [tokens, kv_heads, d] of the cache's type to their slots (int32 [tokens] on the device;
+    negative: not stored)."""
+    shape, device, dtype = k.shape, k.device, k.dtype
+    k_st, v_st = k.stride(), v.stride()
+    if len(shape) != 3 or v.shape != shape or v.dtype != dtype or v.device != device:
+        raise ValueError("k and v must be [tokens, kv_heads, d] of one type and GPU")
+    if device.type != "cuda" or dtype not in _DTYPE_CODES or k_st[2] != 1 or v_st[2] != 1:
+        raise ValueError("k and v must be bfloat16 or float32 on the GPU, d contiguous")
+    n, h, d = shape
+    pages, ch, page, strides = cache._args(d, device, dtype)
+    if ch != h:
+        raise ValueError("k and v must have the cache's heads")
+    _check_ints("slots", slots, n, device)
+    with _here(device, stream):
+        st = lib().sparse_attn_paged_store(n, h, d, _DTYPE_CODES[dtype], k.data_ptr(), _token_strides(shape, k_st),
+                                           v.data_ptr(), _token_strides(shape, v_st), slots.data_ptr(),
+                                           cache.k.data_ptr(), cache.v.data_ptr(), strides, pages, page,
+                                           _stream(stream, device))
+    _check("sparse_attn_paged_store", st)
+    increment_version((cache.k, cache.v))  # written behind torch's back
+
+
+def paged_decode(q, cache: PagedCache, table, positions, stride_l, summary_c, pattern, head_mode, max_pos=None,
+                 softmax_scale=None, out=None, lse=None, workspace=None, stream=None):
+    """Output of one query a sequence (q: [b, h, d], at positions[b], int32 on the device) over the pages that ``table``
+    (int32 [b, max_pages]) names, and its log-sum-exp.  A negative position is a sequence without a query (o = 0, lse =
+    -inf).  ``max_pos``: an upper bound of the positions (default: the table's last); above it o and lse are NaN."""
+    shape, st, device, dtype = q.shape, q.stride(), q.device, q.dtype
+    if len(shape) != 3 or st[2] != 1 or device.type != "cuda" or dtype not in _DTYPE_CODES:
+        raise ValueError("q must be [batch, heads, d] in bfloat16 or float32 on the GPU, d contiguous")
+    b, h, d = shape
+    pages, kv_heads, page, strides = cache._args(d, device, dtype)
+    if kv_heads == 0 or h % kv_heads != 0:
+        raise ValueError("q must have a multiple of the cache's heads")
+    rows, max_pages, table_stride = _check_table(table, device)
+    if rows != b:
+        raise ValueError("table must have a row for each sequence of q")
+    _check_ints("positions", positions, b, device)
+    max_pos = max_pages * page - 1 if max_pos is None else max_pos
+    given = [t for t in (out, lse) if t is not None]  # written behind torch's back
+    code = _DTYPE_CODES[dtype]
+    with _here(device, stream):
+        if out is None:
+            o = torch.empty_like(q)
+            o_st = o.stride()
+        else:
+            o, o_st = out, out.stride()
+            if o.shape != shape or o.dtype != dtype or o.device != device or o_st[2] != 1:
+                raise ValueError("out must match q in shape, type and device, d contiguous")
+        if lse is None:
+            lse = q.new_empty((b, h), dtype=torch.float32)
+        elif lse.shape != (b, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != device:
+            raise ValueError("lse must be a contiguous float32 [batch, heads] tensor on q's device")
+        if workspace is None:
+            size = ctypes.c_size_t()
+            _check("sparse_attn_paged_decode_workspace_size", lib().sparse_attn_paged_decode_workspace_size(
+                max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, code, ctypes.byref(size)))
+            need = size.value
+            workspace = q.new_empty(need, dtype=torch.uint8)
+        else:
+            need = _workspace_bytes(workspace, device)
+        status = lib().sparse_attn_paged_decode(
+            positions.data_ptr(), max_pos, stride_l, summary_c, pattern, head_mode, b, h, kv_heads, d, code, q.data_ptr(),
+            _I64x2(st[0] if b > 1 else 0, st[1] if h > 1 else 0), cache.k.data_ptr(), cache.v.data_ptr(), strides, pages,
+            page, table.data_ptr(), table_stride, max_pages, _scale(softmax_scale, d), o.data_ptr(),
+            _I64x2(o_st[0] if b > 1 else 0, o_st[1] if h > 1 else 0), lse.data_ptr(), workspace.data_ptr(), need,
+            _stream(stream, device))
+    _check("sparse_attn_paged_decode", status)
+    if given:
+        increment_version(given)
+    return o, lse
+
+
+def _workspace_bytes(workspace, device):
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on q's device")
+    return workspace.numel() * workspace.element_size()
+
+
+def packed_forward(q, k, v, starts, stride_l, summary_c, pattern, head_mode, softmax_scale=None, out=None, lse=None,
+                   workspace=None, stream=None):
+    """O [tokens, h, d] and LSE [h, tokens] of sparse attention over sequences packed one behind the other: q [tokens, h,
+    d], k and v [tokens, kv_h, d], sequence s in rows starts[s] .. starts[s + 1] - 1 (int32 [sequences + 1] on the
+    device).  ``stride_l`` from the longest sequence on with SA_STRIDED and SA_MODE_A1 is dense causal attention.  Rows
+    outside all sequences are left as they were in ``out`` and ``lse``.  The result is not differentiable."""
+    shape, device, dtype = q.shape, q.device, q.dtype
+    k_shape, q_st, k_st, v_st = k.shape, q.stride(), k.stride(), v.stride()
+    if len(shape) != 3 or len(k_shape) != 3 or v.shape != k_shape or k_shape[0] != shape[0] or k_shape[2] != shape[2]:
+        raise ValueError("q must be [tokens, heads, d], k and v [tokens, kv_heads, d]")
+    if (device.type != "cuda" or dtype not in _DTYPE_CODES or k.dtype != dtype or v.dtype != dtype or k.device != device
+            or v.device != device):
+        raise ValueError("q, k and v must share type and GPU, in bfloat16 or float32")
+    if q_st[2] != 1 or k_st[2] != 1 or v_st[2] != 1:
+        raise ValueError("q, k and v must have d contiguous")
+    n, h, d = shape
+    if k_shape[1] == 0 or h % k_shape[1] != 0:
+        raise ValueError("q must have a multiple of k's heads")
+    if starts.dim() != 1 or starts.shape[0] < 2:
+        raise ValueError("starts must have an element for each sequence and one behind the last")
+    _check_ints("starts", starts, starts.shape[0], device)
+    given = [t for t in (out, lse) if t is not None]  # written behind torch's back
+    pattern_args = (n, stride_l, summary_c, pattern, head_mode, h, k_shape[1], d, _DTYPE_CODES[dtype])
+    with _here(device, stream):
+        o = q.new_empty(shape) if out is None else out
+        o_st = o.stride()
+        if out is not None and (o.shape != shape or o.dtype != dtype or o.device != device or o_st[2] != 1):
+            raise ValueError("out must match q in shape, type and device, d contiguous")
+        if lse is None:
+            lse = q.new_empty((h, n), dtype=torch.float32)
+        elif lse.shape != (h, n) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != device:
+            raise ValueError("lse must be a contiguous float32 [heads, tokens] tensor on q's device")
+        if workspace is None:
+            size = ctypes.c_size_t()
+            _check("sparse_attn_packed_workspace_size",
+                   lib().sparse_attn_packed_workspace_size(*pattern_args, ctypes.byref(size)))
+            need = size.value
+            workspace = q.new_empty(need, dtype=torch.uint8) if need else None
+        else:
+            need = _workspace_bytes(workspace, device)
+        status = lib().sparse_attn_packed_fwd(
+            starts.shape[0] - 1, starts.data_ptr(), *pattern_args, q.data_ptr(), _token_strides(shape, q_st), k.data_ptr(),
+            _token_strides(k_shape, k_st), v.data_ptr(), _token_strides(k_shape, v_st), _scale(softmax_scale, d),
+            o.data_ptr(), _token_strides(shape, o_st), lse.data_ptr(),
+            None if workspace is None else workspace.data_ptr(), need, _stream(stream, device))
+    _check("sparse_attn_packed_fwd", status)
     if given:
         increment_version(given)
     return o, lse

@@ -1,0 +1,196 @@
+"""The decoding step over pages against 64 bits (bounds: paged_refs.bounds; weights of bf16 in two pieces, 2^-16)."""
+import numpy as np
+import pytest
+import torch
+
+import operator_refs
+import paged_refs as ref
+from paper_1904_10509_amd import sparse_attn as sa
+
+from gpu_util import device, to64
+
+pytestmark = pytest.mark.gpu
+S, F, P = sa.SA_STRIDED, sa.SA_FIXED, sa.SA_FIXED_PER_HEAD
+A1, A2, MG, IL = sa.SA_MODE_A1, sa.SA_MODE_A2, sa.SA_MODE_MERGED, sa.SA_MODE_INTERLEAVED
+BF, FP = torch.bfloat16, torch.float32
+LAST = {BF: 2.0 ** -8, FP: 2.0 ** -24}
+PIECE = {BF: 2.0 ** -16, FP: 0.0}
+
+
+def make(at, kv_heads, capacity, d, dtype, page, seed, interleaved=True):
+    """Pages in no order whose rows behind each sequence's position hold NaN, like the pages that no sequence has; entries
+    of the table behind a sequence's last page point outside the pool."""
+    dev, g = device(), torch.Generator().manual_seed(seed)
+    width = -(-capacity // page)
+    counts = [-(-(p + 1) // page) for p in at]
+    total = sum(counts) + 3
+    order = torch.randperm(total, generator=g)
+    table = torch.full((len(at), width), 10 ** 9)
+    table[:, ::2] = -1
+    k, v = (torch.full((total, kv_heads, page, d), float("nan")) for _ in range(2))
+    first = 0
+    for b, (p, n) in enumerate(zip(at, counts)):
+        table[b, :n] = order[first:first + n]
+        first += n
+        for j in range(n):
+            rows = min(page, p + 1 - j * page)
+            for x in (k, v):
+                x[table[b, j], :, :rows] = torch.randn((kv_heads, rows, d), generator=g)
+    if interleaved:
+        cache = sa.build_paged_cache(total, kv_heads, page, d, dtype, dev)
+    else:
+        cache = sa.PagedCache(*(torch.empty(total, page, kv_heads, d, dtype=dtype, device=dev).transpose(1, 2) for _ in range(2)))
+    cache.k.copy_(k)
+    cache.v.copy_(v)
+    values = [ref.gather(to64(x), table.numpy(), capacity, page) for x in (cache.k, cache.v)]
+    return cache, table.to(torch.int32).to(dev), values
+
+
+def check(o, lse, q, values, at, l, c, pattern, mode, scale=None):
+    d = q.shape[2]
+    want, want_lse, pv, qk, count = operator_refs.decode(to64(q), *values, at, l, c, pattern, mode,
+                                                         d ** -0.5 if scale is None else scale)
+    o_lim, lse_lim = ref.bounds(want, want_lse, pv, qk, count, d, LAST[q.dtype], PIECE[q.dtype])
+    o, ls = to64(o), to64(lse)
+    none = np.isneginf(want_lse)
+    assert np.array_equal(np.isneginf(ls), none) and np.all(o[none] == 0) and np.all(np.isfinite(o))
+    off = np.abs(ls[~none] - want_lse[~none]) - lse_lim[~none]
+    assert np.all(off <= 0), float(off.max())
+    off = np.abs(o - want) - o_lim
+    assert np.all(off <= 0), float(off.max())
+
+
+def places(capacity, l, page):
+    return sorted({0, 1, page - 1, page, l // 2, l - 1, l, l + 1, 2 * l, 3 * l - 1, capacity // 2, capacity - 2, capacity - 1}
+                  & set(range(capacity)))
+
+
+# (pattern, mode, capacity, l, c, d, dtype, heads, kv_heads, page)
+CASES = [
+    (S, MG, 600, 16, 0, 32, FP, 2, 2, 16),
+    (S, A2, 600, 16, 0, 64, FP, 3, 1, 32),
+    (S, MG, 2048, 128, 0, 64, BF, 4, 4, 64),
+    (S, A1, 1000, 100, 0, 64, BF, 4, 2, 128),
+    (S, IL, 777, 31, 0, 128, BF, 6, 2, 16),
+    (S, A1, 3000, 5000, 0, 128, BF, 8, 1, 64),     # dense, eight heads of one key head
+    (S, A1, 3000, 5000, 0, 128, FP, 4, 2, 256),
+    (S, MG, 300, 1, 0, 32, BF, 40, 1, 32),         # every position, forty heads of one key head
+    (F, MG, 4096, 256, 32, 64, BF, 4, 4, 64),
+    (F, A2, 1500, 128, 32, 32, BF, 2, 2, 16),      # empty in the first block
+    (F, IL, 1537, 128, 24, 128, BF, 16, 2, 32),
+    (F, IL, 900, 96, 40, 64, FP, 3, 1, 64),
+    (F, A1, 900, 96, 40, 32, FP, 2, 1, 128),
+    (F, MG, 1100, 48, 48, 128, FP, 20, 4, 64),
+    (P, MG, 2048, 128, 32, 64, BF, 8, 2, 64),
+    (P, A2, 1500, 128, 32, 64, FP, 5, 5, 32),
+    (P, IL, 1000, 48, 12, 128, FP, 16, 2, 16),
+    (P, IL, 640, 20, 6, 32, BF, 12, 1, 128),
+    (P, A2, 400, 32, 16, 32, FP, 70, 2, 16),       # thirty-five heads of one key head, two subblocks
+]
+
+
+@pytest.mark.parametrize("pattern,mode,capacity,l,c,d,dtype,heads,kv_heads,page", CASES)
+def test_paged_decode_matches_64_bits(pattern, mode, capacity, l, c, d, dtype, heads, kv_heads, page):
+    dev = device()
+    at = [-1] + places(capacity, l, page)
+    cache, table, values = make(at, kv_heads, capacity, d, dtype, page, capacity + l + d, interleaved=d != 32)
+    q = torch.randn((len(at), heads, d), generator=torch.Generator().manual_seed(l + d)).to(dtype).to(dev)
+    positions = torch.tensor(at, dtype=torch.int32, device=dev)
+    o, lse = sa.paged_decode(q, cache, table, positions, l, c, pattern, mode)
+    torch.cuda.synchronize()
+    check(o, lse, q, values, at, l, c, pattern, mode)
+    again = sa.paged_decode(q, cache, table, positions, l, c, pattern, mode)
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)
+    few = sa.paged_decode(q, cache, table, positions, l, c, pattern, mode, max_pos=at[4])
+    torch.cuda.synchronize()
+    check(few[0][:5], few[1][:5], q[:5], [x[:5] for x in values], at[:5], l, c, pattern, mode)
+    assert torch.isnan(few[0][5:]).all() and torch.isnan(few[1][5:]).all()  # above the bound
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_pages_that_the_pool_does_not_have(dtype):
+    """NaN for the rows that attend one, and for no other; no address outside the pool is formed."""
+    dev, page, capacity = device(), 16, 400
+    at = [300, 300, 399, 20, -1]
+    for pattern, mode, l, c in ((S, A1, 1000, 0), (S, MG, 32, 0), (F, IL, 64, 16)):
+        cache, table, values = make(at, 2, capacity, 64, dtype, page, 5)
+        q = torch.randn((5, 4, 64), generator=torch.Generator().manual_seed(1)).to(dtype).to(dev)
+        positions = torch.tensor(at, dtype=torch.int32, device=dev)
+        pages = cache.k.shape[0]
+        bad = {(0, 3): pages, (1, 17): -1, (2, 0): 2 ** 31 - 1, (3, 1): -2 ** 31}
+        for (b, i), x in bad.items():
+            table[b, i] = x
+        o, lse = sa.paged_decode(q, cache, table, positions, l, c, pattern, mode)
+        torch.cuda.synchronize()
+        for b, pos in enumerate(at):
+            for h in range(4):
+                keys = operator_refs.attended(pattern, mode, l, c, h, pos) if pos >= 0 else np.array([], int)
+                lost = any(b == bb and np.any(keys // page == i) for bb, i in bad)
+                assert bool(torch.isnan(lse[b, h])) == lost and bool(torch.isnan(o[b, h]).all()) == lost, (b, h)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_infinities_and_nan_among_the_keys(dtype):
+    dev, page, capacity, l = device(), 32, 500, 64
+    at = [499, 499, 499, 130]
+    cache, table, values = make(at, 1, capacity, 64, dtype, page, 9)
+    q = torch.randn((4, 2, 64), generator=torch.Generator().manual_seed(2)).to(dtype).to(dev)
+    positions = torch.tensor(at, dtype=torch.int32, device=dev)
+    args = (l, 0, S, MG)
+    clean = sa.paged_decode(q, cache, table, positions, *args)
+
+    def put(b, pos, which, x):
+        which[table[b, pos // page].item(), 0, pos % page, 7] = x
+    put(0, 480, cache.k, float("nan"))                   # attended
+    put(1, 480, cache.v, float("nan"))
+    put(2, 499 - 3 * l + 1, cache.k, float("nan"))       # not attended
+    put(2, 499 - 3 * l - 1, cache.v, float("inf"))
+    o, lse = sa.paged_decode(q, cache, table, positions, *args)
+    torch.cuda.synchronize()
+    assert torch.isnan(lse[0]).all() and torch.isnan(o[0]).all()
+    assert torch.equal(lse[1], clean[1][1]) and torch.isnan(o[1, :, 7]).all()
+    assert torch.equal(o[1, :, :7], clean[0][1, :, :7]) and torch.equal(o[1, :, 8:], clean[0][1, :, 8:])
+    assert torch.equal(o[2:], clean[0][2:]) and torch.equal(lse[2:], clean[1][2:])
+
+
+def test_strided_views_and_shared_table():
+    """Queries and outputs that are parts of larger tensors, and one table for the whole batch."""
+    dev, page, capacity = device(), 64, 700
+    cache, table, values = make([699], 2, capacity, 64, BF, page, 11)
+    x = torch.randn((3, 12, 64), generator=torch.Generator().manual_seed(3)).to(BF).to(dev)
+    q, out = x[:, 4:8], torch.full((3, 9, 64), 5.0, dtype=BF, device=dev)
+    lse = torch.empty(3, 4, device=dev)
+    positions = torch.tensor([699, 10, 320], dtype=torch.int32, device=dev)
+    shared = table.expand(3, -1)
+    sa.paged_decode(q, cache, shared, positions, 128, 32, F, MG, out=out[:, 2:6], lse=lse)
+    torch.cuda.synchronize()
+    check(out[:, 2:6], lse, q, [np.repeat(v, 3, 0) for v in values], [699, 10, 320], 128, 32, F, MG)
+    assert torch.all(out[:, :2] == 5.0) and torch.all(out[:, 6:] == 5.0)
+
+
+def test_cache_beyond_32_bits():
+    """A pool of more than 4 GiB, pages from both ends of it."""
+    dev, page, d, heads = device(), 256, 128, 2
+    pages = 20000  # 5 GiB
+    kv = torch.empty((pages, heads, page, 2, d), dtype=BF, device=dev)
+    cache = sa.PagedCache(kv[..., 0, :], kv[..., 1, :])
+    table = torch.tensor([[0, pages - 1, pages // 2, 3], [pages - 2, 1, pages - 5, 12000]], dtype=torch.int32, device=dev)
+    for p in table.view(-1).tolist():
+        kv[p] = torch.randn(kv[p].shape, generator=torch.Generator().manual_seed(p)).to(BF).to(dev)
+    values = [np.stack([np.concatenate([to64(x[p]) for p in row], axis=1) for row in table.tolist()]) for x in (cache.k, cache.v)]
+    at = [1000, 900]
+    q = torch.randn((2, 8, d), generator=torch.Generator().manual_seed(4)).to(BF).to(dev)
+    o, lse = sa.paged_decode(q, cache, table, torch.tensor(at, dtype=torch.int32, device=dev), 2000, 0, S, A1)
+    torch.cuda.synchronize()
+    check(o, lse, q, values, at, 2000, 0, S, A1)
+
+
+def test_large_scores():
+    dev = device()
+    for dtype in (BF, FP):
+        cache, table, values = make([399, 100], 2, 400, 64, dtype, 16, 13)
+        q = (8 * torch.randn((2, 4, 64), generator=torch.Generator().manual_seed(5))).to(dtype).to(dev)
+        positions = torch.tensor([399, 100], dtype=torch.int32, device=dev)
+        o, lse = sa.paged_decode(q, cache, table, positions, 1000, 0, S, A1, softmax_scale=1.0)
+        torch.cuda.synchronize()
+        check(o, lse, q, values, [399, 100], 1000, 0, S, A1, scale=1.0)
