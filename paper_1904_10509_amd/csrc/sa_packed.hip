@@ -113,7 +113,9 @@ __device__ inline TilePlace tile_place(const PackedArgs& a, int64_t place, int l
 
 // Consecutive workgroups go to the 8 XCDs in turn: with heads in eighths, an XCD takes neighbouring heads, which
 // share key heads, and their keys stay in its L2.  Places from the last one down: a sequence's longest walks first.
-__device__ inline void place_of(const PackedArgs& a, int64_t id, int64_t* place, int* head) {
+__device__ inline bool place_of(const PackedArgs& a, int64_t* place, int* head) {
+    const int64_t id = blockIdx.x + (int64_t)gridDim.x * blockIdx.y;
+    if (id >= a.places * a.run_heads) return false;
     int h;
     int64_t p;
     if (a.run_heads % 8 == 0) {
@@ -127,6 +129,7 @@ __device__ inline void place_of(const PackedArgs& a, int64_t id, int64_t* place,
     }
     *place = a.places - 1 - p;
     *head = a.head0 + h * a.head_step;
+    return true;
 }
 
 // The walk of a tile of rows i0 .. i1: `far` gathered columns, then the keys lo .. hi.
@@ -213,284 +216,358 @@ __device__ inline int32_t key_row(const PackedArgs& a, int32_t w, const Walk& k,
 }
 
 // ---------------------------------------------------------------------------
-// bf16
+// bf16: waves of 32 rows, 64 keys a step, v_mfma_f32_32x32x16_bf16
 // ---------------------------------------------------------------------------
-// acc += the products of one chunk (operands a, b, see pack_bf16x8) with this lane's row, which attends the
-// rows of the chunk whose bit is set: where a value is an infinity or a NaN, 0 times it would not be 0.
+// With lane = 32 h + r: A operand A[r][8h .. 8h+7], B operand B[8h .. 8h+7][r], D result element i is
+// D[8 (i / 4) + 4 h + i mod 4][r].  S^T = K Q^T leaves a lane 16 of 32 keys of its one query row, and the
+// elements 8 n .. 8 n + 7 are the B operand of P^T for the 16 keys 16 n .. 16 n + 15, if the contraction
+// index 8 h + t stands for key 16 n + 8 (t / 4) + 4 h + t mod 4: V^T is read that way.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+__device__ inline f32x16 mfma_32x32x16(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 zero16() { return f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0}; }
+__device__ inline bf16x8 pack_half(const f32x16& s, int n) {
+    return n == 0 ? pack_bf16x8(f32x4{s[0], s[1], s[2], s[3]}, f32x4{s[4], s[5], s[6], s[7]})
+                  : pack_bf16x8(f32x4{s[8], s[9], s[10], s[11]}, f32x4{s[12], s[13], s[14], s[15]});
+}
+// Max / sum over the two lanes that share r.
+__device__ inline float max_over_h(float x) {
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float sum_over_h(float x) {
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ inline bool non_finite16(const f32x16& x) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t v = __float_as_uint(x[i]) & 0x7FFFFFFFu;
+        top = v > top ? v : top;
+    }
+    return top >= 0x7F800000u;
+}
+
+// acc += the products of 16 keys (operands a, b) with this lane's row, which attends the keys whose bit is set
+// (bits from the first of the 16 on): where a value is an infinity or a NaN, 0 times it would not be 0.
 template <int DB>
-__device__ inline void accumulate_bits(const bf16x8* a, bf16x8 b, uint32_t bits, int g, f32x4* acc) {
+__device__ inline void accumulate_bits(const bf16x8* a, bf16x8 b, uint32_t bits, int h, f32x16* acc) {
     const u32x4 bw = __builtin_bit_cast(u32x4, b);
 #pragma unroll 1
-    for (int x = 0; x < 32; ++x) {  // one row at a time
-        const int e = (x >> 4) * 4 + (x & 3);
+    for (int x = 0; x < 16; ++x) {  // one key at a time
+        const int t = (x >> 3) * 4 + (x & 3);
         u32x4 keep;
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-            keep[y] = g == ((x >> 2) & 3) && y == (e >> 1) ? ((e & 1) ? 0xFFFF0000u : 0xFFFFu) : 0u;
+        for (int y = 0; y < 4; ++y) keep[y] = h == ((x >> 2) & 1) && y == (t >> 1) ? ((t & 1) ? 0xFFFF0000u : 0xFFFFu) : 0u;
         const bf16x8 bx = __builtin_bit_cast(bf16x8, bw & keep);
+        const bool on = (bits >> x) & 1u;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             const bf16x8 ax = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, a[db]) & keep);
-            const f32x4 sum = mfma_16x16x32(ax, bx, acc[db]);
-            if ((bits >> x) & 1u) acc[db] = sum;
+            const f32x16 sum = mfma_32x32x16(ax, bx, acc[db]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] = on ? sum[i] : acc[db][i];
             __builtin_amdgcn_sched_barrier(0);  // one sum in flight: registers
         }
     }
 }
 
-template <int D, bool WIDE>
-struct PackedCfg {
-    static constexpr int QBW = WIDE ? 2 : 1;         // 16-row blocks of a wave
-    static constexpr int RW = 16 * QBW;              // rows of a wave
-    static constexpr int ROWS = RW * kPackedWaves;   // rows of a tile
-    static constexpr int KS = D / 32, DB = D / 16;
-    static constexpr int KB = 4, KC = 2;             // 16-key blocks and 32-key chunks of a step
-    static constexpr int EU = D == 128 ? 2 : 3;      // waves per SIMD
-};
-
-template <int D, bool WIDE, bool FIXED_>
-__global__ void __launch_bounds__(kPackedThreads) __attribute__((amdgpu_waves_per_eu(PackedCfg<D, WIDE>::EU)))
+template <int D, int NW, bool FIXED_>
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3)))
 packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
                    const uint16_t* __restrict__ v, uint16_t* __restrict__ o) {
-    using C = PackedCfg<D, WIDE>;
-    constexpr int KEYS = 64;
+    constexpr int KEYS = 64, ROWS = 32 * NW, KS = D / 16, DB = D / 32;
     __shared__ __attribute__((aligned(16))) uint16_t sK[2][KEYS * D];
     __shared__ __attribute__((aligned(16))) uint16_t sV[2][KEYS * D];
     constexpr uint32_t kTileBytes = KEYS * D * 2;
     const uint32_t sK_base = lds_addr(&sK[0][0]), sV_base = lds_addr(&sV[0][0]);
-    const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, r = lane % 16;
+    const int tid = threadIdx.x, lane = tid % 64, hh = lane / 32, r = lane % 32;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
-    TileReader<D> rd;
-    rd.init(g, r);
     const float c2 = a.scale_log2;
+    // byte offsets of this lane's operand reads in a tile; row blocks of 16 leave the swizzle as it is
+    uint32_t row_off[KS], tr_off[2][DB];
+#pragma unroll
+    for (int x = 0; x < KS; ++x) row_off[x] = 2u * Swz<D>::off(r, 16 * x + 8 * hh);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            tr_off[e][db] = 2u * Swz<D>::off(8 * e + 4 * hh + lane % 16 / 4, 32 * db + 16 * (lane / 16 % 2) + 4 * (lane % 4));
+    // a 1 KiB window of a tile is WR rows; the windows of a wave lie a multiple of 16 rows apart, so that a lane
+    // fetches the same chunk of its row in all of them
+    constexpr int WR = 512 / D, PER = KEYS / WR / NW;
+    static_assert(PER >= 1 && (NW * WR) % 16 == 0, "windows of a wave");
+    const int wrow = lane / (64 / WR), chunk = (lane % (64 / WR)) ^ Swz<D>::perm(w * WR + wrow);
 
-    for (int64_t id = blockIdx.x; id < a.places * a.run_heads; id += gridDim.x) {
-        int64_t place;
-        int h;
-        place_of(a, id, &place, &h);
-        const TilePlace t = tile_place<C::ROWS>(a, place, lane);
-        if (t.n == 0) continue;  // the same for the whole workgroup
-        const int part = FIXED_ ? part_of_head(a.mode, h) : PART_A1;
-        const int32_t win = FIXED_ ? (int32_t)summary_start(a.l, a.c, subblock_of_head(a.sub, h)) : 0;
-        const Walk walk = tile_walk<FIXED_, C::ROWS, KEYS>(a, part, win, t);
-        if (a.put_state && walk.steps == 0) continue;
-        MaskParams mp{FIXED, part, a.l, a.c, 0, 0, 0, win};
-        if (FIXED_ && part == PART_MERGED && a.l <= 64) summary_words(a.l, a.c, win, &mp.sum_lo, &mp.sum_hi);
-        const int row0 = t.i0 + w * C::RW;  // first row of this wave
-        const Row head_row = packed_row<FIXED_>(a, part, win, walk, min(row0, t.n - 1)),
-                  tail_row = packed_row<FIXED_>(a, part, win, walk, min(row0 + C::RW, t.n) - 1);
-        const uint16_t* kh = k + (int64_t)(h / a.group) * a.kh + (int64_t)t.base * a.kt;
-        const uint16_t* vh = v + (int64_t)(h / a.group) * a.vh + (int64_t)t.base * a.vt;
-        const int64_t ks = a.kt * a.step, vs = a.vt * a.step;
+    int64_t place;
+    int h;
+    if (!place_of(a, &place, &h)) return;
+    const TilePlace t = tile_place<ROWS>(a, place, lane);
+    if (t.n == 0) return;  // the same for the whole workgroup
+    const int part = FIXED_ ? part_of_head(a.mode, h) : PART_A1;
+    const int32_t win = FIXED_ ? (int32_t)summary_start(a.l, a.c, subblock_of_head(a.sub, h)) : 0;
+    const Walk walk = tile_walk<FIXED_, ROWS, KEYS>(a, part, win, t);
+    if (a.put_state && walk.steps == 0) return;
+    MaskParams mp{FIXED, part, a.l, a.c, 0, 0, 0, win};
+    if (FIXED_ && part == PART_MERGED && a.l <= 64) summary_words(a.l, a.c, win, &mp.sum_lo, &mp.sum_hi);
+    const int row0 = t.i0 + w * 32;  // first row of this wave
+    const Row head_row = packed_row<FIXED_>(a, part, win, walk, min(row0, t.n - 1)),
+              tail_row = packed_row<FIXED_>(a, part, win, walk, min(row0 + 32, t.n) - 1);
+    const uint16_t* kh = k + (int64_t)(h / a.group) * a.kh + (int64_t)t.base * a.kt;
+    const uint16_t* vh = v + (int64_t)(h / a.group) * a.vh + (int64_t)t.base * a.vt;
+    const int64_t ks = a.kt * a.step, vs = a.vt * a.step;
 
-        bf16x8 qf[C::QBW][C::KS];
-        f32x4 oacc[C::QBW][C::DB];
-        float m_run[C::QBW], l_run[C::QBW];
-        Row rows[C::QBW];
+    const Row row = packed_row<FIXED_>(a, part, win, walk, min(row0 + r, t.n - 1));
+    const int64_t token = t.base + (int64_t)row.i * a.step, at_row = (int64_t)h * a.tokens + token;
+    bf16x8 qf[KS];
+    f32x16 acc[DB];
+    float m_run, l_run;
+    {
+        const uint16_t* p = q + token * a.qt + h * a.qh;
 #pragma unroll
-        for (int u = 0; u < C::QBW; ++u) {
-            rows[u] = packed_row<FIXED_>(a, part, win, walk, min(row0 + 16 * u + r, t.n - 1));
-            const uint16_t* p = q + (t.base + (int64_t)rows[u].i * a.step) * a.qt + h * a.qh;
+        for (int x = 0; x < KS; ++x) qf[x] = ld_bf16x8(p + 16 * x + 8 * hh);
+    }
+    // the state that the rows begin with: nothing, or what the classes left
+    auto begin = [&] {
+        m_run = -INFINITY;
+        l_run = 0.f;
 #pragma unroll
-            for (int x = 0; x < C::KS; ++x) qf[u][x] = ld_bf16x8(p + 32 * x + 8 * g);
-        }
-        // the state that the rows begin with: nothing, or what the classes left
-        auto begin = [&] {
+        for (int db = 0; db < DB; ++db) acc[db] = zero16();
+        if (!FIXED_ && row.i >= a.state_from) {
+            m_run = a.state_ml[2 * at_row];
+            l_run = hh == 0 ? a.state_ml[2 * at_row + 1] : 0.f;
 #pragma unroll
-            for (int u = 0; u < C::QBW; ++u) {
-                m_run[u] = -INFINITY;
-                l_run[u] = 0.f;
+            for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int db = 0; db < C::DB; ++db) oacc[u][db] = zero4();
-                if (!FIXED_ && rows[u].i >= a.state_from) {
-                    const int64_t at = (int64_t)h * a.tokens + t.base + rows[u].i;
-                    m_run[u] = a.state_ml[2 * at];
-                    l_run[u] = g == 0 ? a.state_ml[2 * at + 1] : 0.f;
+                for (int y = 0; y < 4; ++y) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(a.state_o + at_row * D + 32 * db + 8 * y + 4 * hh);
 #pragma unroll
-                    for (int db = 0; db < C::DB; ++db)
-                        oacc[u][db] = *reinterpret_cast<const f32x4*>(a.state_o + at * D + 16 * db + 4 * g);
+                    for (int i = 0; i < 4; ++i) acc[db][4 * y + i] = x[i];
                 }
-            }
-        };
-        // one step's K and V rows to a ring stage: lane L of window `win` fetches the chunk that belongs at its slot
-        constexpr int PER = KEYS * D / 512 / kPackedWaves;  // 1 KiB windows of a wave and tile
-        auto load_step = [&](int e, int stage) {
+        }
+    };
+    // one step's K and V rows to a ring stage.  Where a window's rows follow each other and exist, its address
+    // is one scalar; else every lane forms its row's.
+    const bool near_offsets = 32 * max64(ks, vs) < (int64_t)1 << 31;
+    const bool far_runs = FIXED_ && a.c % WR == 0;
+    const uint32_t k_off = (uint32_t)((wrow * ks + 8 * chunk) * 2), v_off = (uint32_t)((wrow * vs + 8 * chunk) * 2);
+    auto load_step = [&](int e, int stage) {
+        const bool far = FIXED_ && e < walk.far_steps;
+        const int32_t first = far ? KEYS * e : walk.lo + KEYS * (e - walk.far_steps);
+        const bool whole = near_offsets && (far ? far_runs && first + KEYS <= walk.far : first + KEYS <= t.n);
+        const uint32_t kdst = sK_base + stage * kTileBytes, vdst = sV_base + stage * kTileBytes;
+        if (whole) {
 #pragma unroll
             for (int x = 0; x < PER; ++x) {
-                const int window = w + kPackedWaves * x, oe = 512 * window + 8 * lane;
-                const int at = oe / D, chunk = ((oe % D) / 8) ^ Swz<D>::perm(at);
-                const int64_t j = key_row<FIXED_, KEYS>(a, win, walk, e, at);
-                dma_b128_at(kh + j * ks + 8 * chunk, sK_base + stage * kTileBytes + 1024 * window);
-                dma_b128_at(vh + j * vs + 8 * chunk, sV_base + stage * kTileBytes + 1024 * window);
+                const int window = w + NW * x;
+                const int64_t j = __builtin_amdgcn_readfirstlane(
+                    far ? key_row<FIXED_, KEYS>(a, win, walk, e, WR * window) : first + WR * window);
+                dma_b128(uniform_ptr(kh + j * ks), k_off, kdst + 1024 * window);
+                dma_b128(uniform_ptr(vh + j * vs), v_off, vdst + 1024 * window);
             }
-        };
-
-        bool careful = false;
-        while (true) {
-            begin();
-            // (no load that the compiler tracks is left inside the loop: a wait for one would drain the ring)
-            wait_loads_upto<0>();
-            if (walk.steps > 0) load_step(0, 0);
-            int e = 0;
-            two_stage_while([&](auto stage) {
-                constexpr int st = decltype(stage)::value;
-                if (e >= walk.steps) return false;
-                wait_loads_upto<0>();
-                __syncthreads();  // this step is in LDS everywhere; the other stage is free
-                if (e + 1 < walk.steps) load_step(e + 1, st ^ 1);
-                const uint16_t* tK = sK[st];
-                const uint16_t* tV = sV[st];
-                auto compute = [&](auto full) {
-                    uint64_t bits[C::QBW];
-                    int cls[C::QBW][C::KC];
+        } else {
 #pragma unroll
-                    for (int u = 0; u < C::QBW; ++u) {
-                        bits[u] = ~0ull;
-#pragma unroll
-                        for (int kc = 0; kc < C::KC; ++kc) cls[u][kc] = CHUNK_ALL;
-                    }
-                    if constexpr (!decltype(full)::value) {
-                        const int32_t j0 = walk.lo + KEYS * (e - walk.far_steps);
-                        uint64_t sum = 0;
-                        if (FIXED_ && part == PART_MERGED && e >= walk.far_steps) sum = summary_bits(mp, mod_l(a.dl, j0));
-#pragma unroll
-                        for (int u = 0; u < C::QBW; ++u) {
-                            bits[u] = row_bits<FIXED_, KEYS>(a, part, walk, rows[u], e, sum);
-#pragma unroll
-                            for (int kc = 0; kc < C::KC; ++kc)
-                                cls[u][kc] = chunk_class(chunk_bits(bits[u] >> (4 * g), kc, true), true);
-                        }
-                    }
-                    bool live[C::KC];
-#pragma unroll
-                    for (int kc = 0; kc < C::KC; ++kc) {
-                        live[kc] = false;
-#pragma unroll
-                        for (int u = 0; u < C::QBW; ++u) live[kc] = live[kc] || cls[u][kc] != CHUNK_NONE;
-                    }
-                    // V^T operands, read now: their latency hides behind the products and the softmax
-                    bf16x8 vt[C::KC][C::DB];
-#pragma unroll
-                    for (int kc = 0; kc < C::KC; ++kc) {
-                        if (!live[kc]) continue;
-#pragma unroll
-                        for (int db = 0; db < C::DB; ++db) vt[kc][db] = rd.tr(tV, kc * 32, kc * 32 + 16, db);
-                    }
-                    __builtin_amdgcn_s_setprio(1);
-                    f32x4 s[C::QBW][C::KB];
-#pragma unroll
-                    for (int kb = 0; kb < C::KB; ++kb) {
-#pragma unroll
-                        for (int u = 0; u < C::QBW; ++u) s[u][kb] = zero4();
-                        if (!live[kb / 2]) continue;
-                        bf16x8 kf[C::KS];
-#pragma unroll
-                        for (int x = 0; x < C::KS; ++x) kf[x] = rd.row(tK, kb * 16, x);
-#pragma unroll
-                        for (int u = 0; u < C::QBW; ++u) {
-                            if (cls[u][kb / 2] == CHUNK_NONE) continue;
-#pragma unroll
-                            for (int x = 0; x < C::KS; ++x) s[u][kb] = mfma_16x16x32(kf[x], qf[u][x], s[u][kb]);
-                        }
-                    }
-                    __builtin_amdgcn_s_setprio(0);
-#pragma unroll
-                    for (int u = 0; u < C::QBW; ++u) {
-                        float mloc = -INFINITY;
-#pragma unroll
-                        for (int kc = 0; kc < C::KC; ++kc) {
-                            if (cls[u][kc] == CHUNK_NONE) continue;
-                            if (cls[u][kc] == CHUNK_PART) {
-#pragma unroll
-                                for (int hk = 0; hk < 2; ++hk)
-#pragma unroll
-                                    for (int y = 0; y < 4; ++y)
-                                        s[u][2 * kc + hk][y] = select_or_neg_inf(
-                                            bit_lane_mask(bits[u] >> (4 * g), 16 * (2 * kc + hk) + y), s[u][2 * kc + hk][y]);
-                            }
-#pragma unroll
-                            for (int hk = 0; hk < 2; ++hk) {
-                                const f32x4 x = s[u][2 * kc + hk];
-                                mloc = fmaxf(fmaxf(mloc, x[0]), x[1]);
-                                mloc = fmaxf(fmaxf(mloc, x[2]), x[3]);
-                            }
-                        }
-                        mloc = max_over_g(mloc);
-                        const float m_new = fmaxf(m_run[u], mloc);
-                        // rows with nothing attended so far keep m = -inf; 0 as reference gives p = 0
-                        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-                        const float neg = -m_ref * c2;
-                        float psum = 0.f;
-                        bf16x8 pf[C::KC];
-#pragma unroll
-                        for (int kc = 0; kc < C::KC; ++kc) {
-                            if (cls[u][kc] != CHUNK_NONE) {
-#pragma unroll
-                                for (int hk = 0; hk < 2; ++hk)
-#pragma unroll
-                                    for (int y = 0; y < 4; ++y) {
-                                        const float p = exp2_fast(fmaf(s[u][2 * kc + hk][y], c2, neg));
-                                        s[u][2 * kc + hk][y] = p;
-                                        psum += p;
-                                    }
-                            }
-                            // weights rounded to bf16 for the matrix product, 2^-9 of each; the sum takes them whole
-                            pf[kc] = pack_bf16x8(s[u][2 * kc], s[u][2 * kc + 1]);
-                        }
-                        const float alpha = exp2_fast((m_run[u] - m_ref) * c2);
-                        l_run[u] = fmaf(l_run[u], alpha, psum);
-                        m_run[u] = m_new;
-#pragma unroll
-                        for (int db = 0; db < C::DB; ++db) oacc[u][db] *= alpha;
-#pragma unroll
-                        for (int kc = 0; kc < C::KC; ++kc) {
-                            if (cls[u][kc] == CHUNK_NONE) continue;
-                            if (!decltype(full)::value && careful && cls[u][kc] == CHUNK_PART) {
-                                accumulate_bits<C::DB>(vt[kc], pf[kc], (uint32_t)(bits[u] >> (32 * kc)), g, oacc[u]);
-                                continue;
-                            }
-#pragma unroll
-                            for (int db = 0; db < C::DB; ++db) oacc[u][db] = mfma_16x16x32(vt[kc][db], pf[kc], oacc[u][db]);
-                        }
-                    }
-                };
-                if (step_full<FIXED_, KEYS>(a, part, walk, e, head_row, tail_row)) compute(std::true_type{});
-                else compute(std::false_type{});
-                ++e;
-                return true;
-            });
-            // an infinity or a NaN in a key that a row does not attend must not reach it: such sums are formed
-            // a second time, with the products of partly attended chunks kept apart by row
-            bool bad = false;
-#pragma unroll
-            for (int u = 0; u < C::QBW; ++u) bad = bad || non_finite<C::DB>(oacc[u]);
-            if (!__syncthreads_or(bad) || careful) break;
-            careful = true;
+            for (int x = 0; x < PER; ++x) {
+                const int window = w + NW * x;
+                const int64_t j = key_row<FIXED_, KEYS>(a, win, walk, e, WR * window + wrow);
+                dma_b128_at(kh + j * ks + 8 * chunk, kdst + 1024 * window);
+                dma_b128_at(vh + j * vs + 8 * chunk, vdst + 1024 * window);
+            }
         }
+    };
 
+    // V^T operand of 16 keys: columns 32 db + r
+    auto values = [&](const char* at, int db) {
+        const u32x2 lo = ld_tr16(reinterpret_cast<const uint16_t*>(at + tr_off[0][db]));
+        const u32x2 hi = ld_tr16(reinterpret_cast<const uint16_t*>(at + tr_off[1][db]));
+        return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
+    };
+    begin();
+    // (no load that the compiler tracks is left inside the loop: a wait for one would drain the ring)
+    wait_loads_upto<0>();
+    if (walk.steps > 0) load_step(0, 0);
+    int e = 0;
+    two_stage_while([&](auto stage) {
+        constexpr int st = decltype(stage)::value;
+        if (e >= walk.steps) return false;
+        wait_loads_upto<0>();
+        __syncthreads();  // this step is in LDS everywhere; the other stage is free
+        if (e + 1 < walk.steps) load_step(e + 1, st ^ 1);
+        const char* tK = reinterpret_cast<const char*>(sK[st]);
+        const char* tV = reinterpret_cast<const char*>(sV[st]);
+        auto compute = [&](auto full) {
+            uint64_t bits = ~0ull;
+            int cls[2] = {CHUNK_ALL, CHUNK_ALL};
+            if constexpr (!decltype(full)::value) {
+                const int32_t j0 = walk.lo + KEYS * (e - walk.far_steps);
+                uint64_t sum = 0;
+                if (FIXED_ && part == PART_MERGED && e >= walk.far_steps) sum = summary_bits(mp, mod_l(a.dl, j0));
+                bits = row_bits<FIXED_, KEYS>(a, part, walk, row, e, sum);
 #pragma unroll
-        for (int u = 0; u < C::QBW; ++u) {
-            const float l_tot = sum_over_g(l_run[u]);
-            if (row0 + 16 * u + r >= t.n) continue;
-            const int64_t token = t.base + (int64_t)rows[u].i * a.step, at = (int64_t)h * a.tokens + token;
-            if (a.put_state) {
-                if (rows[u].i < a.shift) continue;  // no key: the band begins with nothing there
-#pragma unroll
-                for (int db = 0; db < C::DB; ++db)
-                    *reinterpret_cast<f32x4*>(a.state_o + at * D + 16 * db + 4 * g) = oacc[u][db];
-                if (g == 0) {
-                    a.state_ml[2 * at] = m_run[u];
-                    a.state_ml[2 * at + 1] = l_tot;
+                for (int kb = 0; kb < 2; ++kb) {
+                    const uint32_t b = (uint32_t)(bits >> (32 * kb));
+                    cls[kb] = __builtin_amdgcn_ballot_w64(b != 0u) == 0ull    ? CHUNK_NONE
+                              : __builtin_amdgcn_ballot_w64(b != ~0u) == 0ull ? CHUNK_ALL
+                                                                              : CHUNK_PART;
                 }
-                continue;
+                if (cls[0] == CHUNK_NONE && cls[1] == CHUNK_NONE) return;
             }
+            f32x16 s[2];
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                s[kb] = zero16();
+                if (cls[kb] == CHUNK_NONE) continue;
+#pragma unroll
+                for (int x = 0; x < KS; ++x)
+                    s[kb] = mfma_32x32x16(
+                        ld_bf16x8(reinterpret_cast<const uint16_t*>(tK + row_off[x] + kb * 32 * D * 2)), qf[x], s[kb]);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            float mloc = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                if (cls[kb] == CHUNK_NONE) continue;
+                if (cls[kb] == CHUNK_PART) {
+                    const uint32_t b = (uint32_t)(bits >> (32 * kb)) >> (4 * hh);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        s[kb][i] = select_or_neg_inf(bit_lane_mask(b, 8 * (i / 4) + i % 4), s[kb][i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) mloc = fmaxf(fmaxf(mloc, s[kb][i]), s[kb][i + 1]);
+            }
+            mloc = max_over_h(mloc);
+            const float m_new = fmaxf(m_run, mloc);
+            // rows with nothing attended so far keep m = -inf; 0 as reference gives p = 0
+            const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+            const float neg = -m_ref * c2;
+            const float alpha = exp2_fast((m_run - m_ref) * c2);
+            m_run = m_new;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+            float psum = 0.f;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                if (cls[kb] == CHUNK_NONE) continue;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[kb][i] = exp2_fast(fmaf(s[kb][i], c2, neg));
+                    psum += s[kb][i];
+                }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    // weights rounded to bf16 for the matrix product, 2^-9 of each; the sum takes them whole
+                    const bf16x8 pf = pack_half(s[kb], n);
+                    bf16x8 vt[DB];
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) vt[db] = values(tV + (32 * kb + 16 * n) * D * 2, db);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) acc[db] = mfma_32x32x16(vt[db], pf, acc[db]);
+                }
+            }
+            l_run = fmaf(l_run, alpha, psum);
+        };
+        if (step_full<FIXED_, KEYS>(a, part, walk, e, head_row, tail_row)) compute(std::true_type{});
+        else compute(std::false_type{});
+        ++e;
+        return true;
+    });
+    // An infinity or a NaN in a key that a row does not attend must not reach it, but 0 times it is not 0: sums that
+    // come out non-finite are formed a second time, with the products of partly attended chunks kept apart by row.
+    bool bad = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) bad = bad || non_finite16(acc[db]);
+    if (__syncthreads_or(bad)) {
+        begin();
+#pragma unroll 1
+        for (int e = 0; e < walk.steps; ++e) {
+            load_step(e, 0);
+            wait_loads_upto<0>();
+            __syncthreads();
+            const int32_t j0 = walk.lo + KEYS * (e - walk.far_steps);
+            uint64_t sum = 0;
+            if (FIXED_ && part == PART_MERGED && e >= walk.far_steps) sum = summary_bits(mp, mod_l(a.dl, j0));
+            const uint64_t bits = row_bits<FIXED_, KEYS>(a, part, walk, row, e, sum);
+            if (__builtin_amdgcn_ballot_w64(bits != 0ull) != 0ull) {
+                f32x16 s[2];
+                float mloc = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const char* tK = reinterpret_cast<const char*>(sK[0]) + kb * 32 * D * 2;
+                    s[kb] = zero16();
+#pragma unroll
+                    for (int x = 0; x < KS; ++x)
+                        s[kb] = mfma_32x32x16(ld_bf16x8(reinterpret_cast<const uint16_t*>(tK + row_off[x])), qf[x], s[kb]);
+                    const uint32_t b = (uint32_t)(bits >> (32 * kb)) >> (4 * hh);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[kb][i] = select_or_neg_inf(bit_lane_mask(b, 8 * (i / 4) + i % 4), s[kb][i]);
+                        mloc = fmaxf(mloc, s[kb][i]);
+                    }
+                }
+                const float m_new = fmaxf(m_run, max_over_h(mloc)), m_ref = m_new == -INFINITY ? 0.f : m_new;
+                const float alpha = exp2_fast((m_run - m_ref) * c2);
+                m_run = m_new;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+                float psum = 0.f;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const uint32_t b = (uint32_t)(bits >> (32 * kb));
+                    const bool all = __builtin_amdgcn_ballot_w64(b != ~0u) == 0ull;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[kb][i] = exp2_fast(fmaf(s[kb][i], c2, -m_ref * c2));
+                        psum += s[kb][i];
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const bf16x8 pf = pack_half(s[kb], n);
+                        bf16x8 vt[DB];
+#pragma unroll
+                        for (int db = 0; db < DB; ++db)
+                            vt[db] = values(reinterpret_cast<const char*>(sV[0]) + (32 * kb + 16 * n) * D * 2, db);
+                        if (all) {
+#pragma unroll
+                            for (int db = 0; db < DB; ++db) acc[db] = mfma_32x32x16(vt[db], pf, acc[db]);
+                        } else {
+                            accumulate_bits<DB>(vt, pf, b >> (16 * n), hh, acc);
+                        }
+                    }
+                }
+                l_run = fmaf(l_run, alpha, psum);
+            }
+            __syncthreads();  // read before the next step is written
+        }
+    }
+
+    const float l_tot = sum_over_h(l_run);
+    if (row0 + r < t.n) {
+        if (!a.put_state) {
             const bool none = no_key(l_tot);
             const float inv = none ? 0.f : 1.f / l_tot;
             uint16_t* orow = o + token * a.ot + h * a.oh;
 #pragma unroll
-            for (int db = 0; db < C::DB; ++db)
-                *reinterpret_cast<uint2*>(orow + db * 16 + 4 * g) = pack_bf16x4_bits(oacc[u][db] * inv);
-            if (g == 0) a.lse[at] = none ? -INFINITY : (m_run[u] * c2 + __log2f(l_tot)) / kLog2e;
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    *reinterpret_cast<uint2*>(orow + 32 * db + 8 * y + 4 * hh) = pack_bf16x4_bits(
+                        f32x4{acc[db][4 * y], acc[db][4 * y + 1], acc[db][4 * y + 2], acc[db][4 * y + 3]} * inv);
+            if (hh == 0) a.lse[at_row] = none ? -INFINITY : (m_run * c2 + __log2f(l_tot)) / kLog2e;
+        } else if (row.i >= a.shift) {  // (no key before: the band begins with nothing there)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    *reinterpret_cast<f32x4*>(a.state_o + at_row * D + 32 * db + 8 * y + 4 * hh) =
+                        f32x4{acc[db][4 * y], acc[db][4 * y + 1], acc[db][4 * y + 2], acc[db][4 * y + 3]};
+            if (hh == 0) {
+                a.state_ml[2 * at_row] = m_run;
+                a.state_ml[2 * at_row + 1] = l_tot;
+            }
         }
     }
 }
@@ -524,191 +601,194 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
     const float c2 = a.scale_log2;
 
-    for (int64_t id = blockIdx.x; id < a.places * a.run_heads; id += gridDim.x) {
-        int64_t place;
-        int h;
-        place_of(a, id, &place, &h);
-        const TilePlace t = tile_place<ROWS>(a, place, lane);
-        if (t.n == 0) continue;
-        const int part = FIXED_ ? part_of_head(a.mode, h) : PART_A1;
-        const int32_t win = FIXED_ ? (int32_t)summary_start(a.l, a.c, subblock_of_head(a.sub, h)) : 0;
-        const Walk walk = tile_walk<FIXED_, ROWS, KEYS>(a, part, win, t);
-        if (a.put_state && walk.steps == 0) continue;
-        MaskParams mp{FIXED, part, a.l, a.c, 0, 0, 0, win};
-        if (FIXED_ && part == PART_MERGED && a.l <= 64) summary_words(a.l, a.c, win, &mp.sum_lo, &mp.sum_hi);
-        const int row0 = t.i0 + w * 16;
-        const Row head_row = packed_row<FIXED_>(a, part, win, walk, min(row0, t.n - 1)),
-                  tail_row = packed_row<FIXED_>(a, part, win, walk, min(row0 + 16, t.n) - 1);
-        const float* kh = k + (int64_t)(h / a.group) * a.kh + (int64_t)t.base * a.kt;
-        const float* vh = v + (int64_t)(h / a.group) * a.vh + (int64_t)t.base * a.vt;
-        const int64_t ks = a.kt * a.step, vs = a.vt * a.step;
+    int64_t place;
+    int h;
+    if (!place_of(a, &place, &h)) return;
+    const TilePlace t = tile_place<ROWS>(a, place, lane);
+    if (t.n == 0) return;  // the same for the whole workgroup
+    const int part = FIXED_ ? part_of_head(a.mode, h) : PART_A1;
+    const int32_t win = FIXED_ ? (int32_t)summary_start(a.l, a.c, subblock_of_head(a.sub, h)) : 0;
+    const Walk walk = tile_walk<FIXED_, ROWS, KEYS>(a, part, win, t);
+    if (a.put_state && walk.steps == 0) return;
+    MaskParams mp{FIXED, part, a.l, a.c, 0, 0, 0, win};
+    if (FIXED_ && part == PART_MERGED && a.l <= 64) summary_words(a.l, a.c, win, &mp.sum_lo, &mp.sum_hi);
+    const int row0 = t.i0 + w * 16;
+    const Row head_row = packed_row<FIXED_>(a, part, win, walk, min(row0, t.n - 1)),
+              tail_row = packed_row<FIXED_>(a, part, win, walk, min(row0 + 16, t.n) - 1);
+    const float* kh = k + (int64_t)(h / a.group) * a.kh + (int64_t)t.base * a.kt;
+    const float* vh = v + (int64_t)(h / a.group) * a.vh + (int64_t)t.base * a.vt;
+    const int64_t ks = a.kt * a.step, vs = a.vt * a.step;
 
-        const Row row = packed_row<FIXED_>(a, part, win, walk, min(row0 + r, t.n - 1));
-        const int64_t token = t.base + (int64_t)row.i * a.step, at_row = (int64_t)h * a.tokens + token;
-        f32x4 qf[DB], acc[DB];
-        float m_run, l_run;
-        {
-            const float* p = q + token * a.qt + h * a.qh;
+    const Row row = packed_row<FIXED_>(a, part, win, walk, min(row0 + r, t.n - 1));
+    const int64_t token = t.base + (int64_t)row.i * a.step, at_row = (int64_t)h * a.tokens + token;
+    f32x4 qf[DB], acc[DB];
+    float m_run, l_run;
+    {
+        const float* p = q + token * a.qt + h * a.qh;
 #pragma unroll
-            for (int x = 0; x < DB; ++x) qf[x] = *reinterpret_cast<const f32x4*>(p + 16 * x + 4 * g);
+        for (int x = 0; x < DB; ++x) qf[x] = *reinterpret_cast<const f32x4*>(p + 16 * x + 4 * g);
+    }
+    // acc[V hb + e][i] is element 16 V hb + V (4 g + i) + e
+    auto begin = [&] {
+        m_run = -INFINITY;
+        l_run = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = zero4();
+        if (!FIXED_ && row.i >= a.state_from) {
+            m_run = a.state_ml[2 * at_row];
+            l_run = g == 0 ? a.state_ml[2 * at_row + 1] : 0.f;
+#pragma unroll
+            for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const vec x = *reinterpret_cast<const vec*>(a.state_o + at_row * D + 16 * V * hb + V * (4 * g + i));
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[V * hb + e][i] = x[e];
+                }
         }
-        // acc[V hb + e][i] is element 16 V hb + V (4 g + i) + e
-        auto begin = [&] {
-            m_run = -INFINITY;
-            l_run = 0.f;
+    };
+    constexpr int PER = KEYS * D / 256 / kPackedWaves;
+    auto load_step = [&](int e, int stage) {
 #pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] = zero4();
-            if (!FIXED_ && row.i >= a.state_from) {
-                m_run = a.state_ml[2 * at_row];
-                l_run = g == 0 ? a.state_ml[2 * at_row + 1] : 0.f;
+        for (int x = 0; x < PER; ++x) {
+            const int window = w + kPackedWaves * x, oe = 256 * window + 4 * lane;
+            const int at = oe / D, piece = swz32<D>(at, (oe % D) / 4);
+            const int64_t j = key_row<FIXED_, KEYS>(a, win, walk, e, at);
+            dma_b128_at(kh + j * ks + 4 * piece, sK_base + stage * kTileBytes + 1024 * window);
+            dma_b128_at(vh + j * vs + 4 * piece, sV_base + stage * kTileBytes + 1024 * window);
+        }
+    };
+
+    bool careful = false;
+    while (true) {
+        begin();
+        wait_loads_upto<0>();
+        if (walk.steps > 0) load_step(0, 0);
+        int e = 0;
+        two_stage_while([&](auto stage) {
+            constexpr int st = decltype(stage)::value;
+            if (e >= walk.steps) return false;
+            wait_loads_upto<0>();
+            __syncthreads();
+            if (e + 1 < walk.steps) load_step(e + 1, st ^ 1);
+            const float* tK = sK[st];
+            const float* tV = sV[st];
+            uint32_t bits = ~0u;
+            if (!step_full<FIXED_, KEYS>(a, part, walk, e, head_row, tail_row)) {
+                const int32_t j0 = walk.lo + KEYS * (e - walk.far_steps);
+                uint64_t sum = 0;
+                if (FIXED_ && part == PART_MERGED && e >= walk.far_steps) sum = summary_bits(mp, mod_l(a.dl, j0));
+                bits = (uint32_t)row_bits<FIXED_, KEYS>(a, part, walk, row, e, sum);
+            }
+            if (__builtin_amdgcn_ballot_w64(bits != 0u) != 0ull) {
+                f32x4 s[2];
 #pragma unroll
-                for (int hb = 0; hb < HB; ++hb)
+                for (int y = 0; y < 2; ++y) {  // key 16 y + 4 g + i
+                    f32x4 c0 = zero4(), c1 = zero4();
+#pragma unroll
+                    for (int x = 0; x < DB; ++x) {
+                        const f32x4 kf =
+                            *reinterpret_cast<const f32x4*>(tK + (16 * y + r) * D + 4 * swz32<D>(16 * y + r, 4 * x + g));
+                        c0 = mfma_f32(kf[0], qf[x][0], c0);
+                        c1 = mfma_f32(kf[1], qf[x][1], c1);
+                        c0 = mfma_f32(kf[2], qf[x][2], c0);
+                        c1 = mfma_f32(kf[3], qf[x][3], c1);
+                    }
+                    s[y] = c0 + c1;
+                }
+                float mx = m_run;
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const vec x = *reinterpret_cast<const vec*>(a.state_o + at_row * D + 16 * V * hb + V * (4 * g + i));
-#pragma unroll
-                        for (int e = 0; e < V; ++e) acc[V * hb + e][i] = x[e];
+                        s[y][i] = select_or_neg_inf(bit_lane_mask(bits >> (4 * g), 16 * y + i), s[y][i]);
+                        mx = fmaxf(mx, s[y][i]);
                     }
-            }
-        };
-        constexpr int PER = KEYS * D / 256 / kPackedWaves;
-        auto load_step = [&](int e, int stage) {
+                mx = max_over_g(mx);
+                const float m_ref = mx == -INFINITY ? 0.f : mx;
+                const float alpha = exp2_fast((m_run - m_ref) * c2);
+                float psum = 0.f;
+                // (the difference first: scaling before would lose 2^-24 of the scores themselves)
 #pragma unroll
-            for (int x = 0; x < PER; ++x) {
-                const int window = w + kPackedWaves * x, oe = 256 * window + 4 * lane;
-                const int at = oe / D, piece = swz32<D>(at, (oe % D) / 4);
-                const int64_t j = key_row<FIXED_, KEYS>(a, win, walk, e, at);
-                dma_b128_at(kh + j * ks + 4 * piece, sK_base + stage * kTileBytes + 1024 * window);
-                dma_b128_at(vh + j * vs + 4 * piece, sV_base + stage * kTileBytes + 1024 * window);
-            }
-        };
-
-        bool careful = false;
-        while (true) {
-            begin();
-            wait_loads_upto<0>();
-            if (walk.steps > 0) load_step(0, 0);
-            int e = 0;
-            two_stage_while([&](auto stage) {
-                constexpr int st = decltype(stage)::value;
-                if (e >= walk.steps) return false;
-                wait_loads_upto<0>();
-                __syncthreads();
-                if (e + 1 < walk.steps) load_step(e + 1, st ^ 1);
-                const float* tK = sK[st];
-                const float* tV = sV[st];
-                uint32_t bits = ~0u;
-                if (!step_full<FIXED_, KEYS>(a, part, walk, e, head_row, tail_row)) {
-                    const int32_t j0 = walk.lo + KEYS * (e - walk.far_steps);
-                    uint64_t sum = 0;
-                    if (FIXED_ && part == PART_MERGED && e >= walk.far_steps) sum = summary_bits(mp, mod_l(a.dl, j0));
-                    bits = (uint32_t)row_bits<FIXED_, KEYS>(a, part, walk, row, e, sum);
-                }
-                if (__builtin_amdgcn_ballot_w64(bits != 0u) != 0ull) {
-                    f32x4 s[2];
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {  // key 16 y + 4 g + i
-                        f32x4 c0 = zero4(), c1 = zero4();
-#pragma unroll
-                        for (int x = 0; x < DB; ++x) {
-                            const f32x4 kf =
-                                *reinterpret_cast<const f32x4*>(tK + (16 * y + r) * D + 4 * swz32<D>(16 * y + r, 4 * x + g));
-                            c0 = mfma_f32(kf[0], qf[x][0], c0);
-                            c1 = mfma_f32(kf[1], qf[x][1], c1);
-                            c0 = mfma_f32(kf[2], qf[x][2], c0);
-                            c1 = mfma_f32(kf[3], qf[x][3], c1);
-                        }
-                        s[y] = c0 + c1;
+                    for (int i = 0; i < 4; ++i) {
+                        s[y][i] = exp2_fast((s[y][i] - m_ref) * c2);
+                        psum += s[y][i];
                     }
-                    float mx = m_run;
+                l_run = fmaf(l_run, alpha, psum);
+                m_run = mx;
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                for (int db = 0; db < DB; ++db) acc[db] *= alpha;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            s[y][i] = select_or_neg_inf(bit_lane_mask(bits >> (4 * g), 16 * y + i), s[y][i]);
-                            mx = fmaxf(mx, s[y][i]);
-                        }
-                    mx = max_over_g(mx);
-                    const float m_ref = mx == -INFINITY ? 0.f : mx;
-                    const float alpha = exp2_fast((m_run - m_ref) * c2);
-                    float psum = 0.f;
-                    // (the difference first: scaling before would lose 2^-24 of the scores themselves)
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = 16 * y + 4 * g + i;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            s[y][i] = exp2_fast((s[y][i] - m_ref) * c2);
-                            psum += s[y][i];
-                        }
-                    l_run = fmaf(l_run, alpha, psum);
-                    m_run = mx;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) acc[db] *= alpha;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = 16 * y + 4 * g + i;
-#pragma unroll
-                            for (int hb = 0; hb < HB; ++hb) {
-                                const int col = 16 * V * hb + V * r;
-                                const vec x = *reinterpret_cast<const vec*>(tV + key * D + 4 * swz32<D>(key, col / 4) + col % 4);
-                                if (careful) {  // one key at a time, for the rows that attend it
+                        for (int hb = 0; hb < HB; ++hb) {
+                            const int col = 16 * V * hb + V * r;
+                            const vec x = *reinterpret_cast<const vec*>(tV + key * D + 4 * swz32<D>(key, col / 4) + col % 4);
+                            if (careful) {  // one key at a time, for the rows that attend it
 #pragma unroll 1
-                                    for (int gk = 0; gk < 4; ++gk) {
-                                        const bool on = (bits >> (16 * y + 4 * gk + i)) & 1u;
+                                for (int gk = 0; gk < 4; ++gk) {
+                                    const bool on = (bits >> (16 * y + 4 * gk + i)) & 1u;
 #pragma unroll
-                                        for (int e = 0; e < V; ++e) {
-                                            const f32x4 sum =
-                                                mfma_f32(g == gk ? x[e] : 0.f, g == gk ? s[y][i] : 0.f, acc[V * hb + e]);
-                                            if (on) acc[V * hb + e] = sum;
-                                        }
+                                    for (int e = 0; e < V; ++e) {
+                                        const f32x4 sum =
+                                            mfma_f32(g == gk ? x[e] : 0.f, g == gk ? s[y][i] : 0.f, acc[V * hb + e]);
+                                        if (on) acc[V * hb + e] = sum;
                                     }
-                                } else {
-#pragma unroll
-                                    for (int e = 0; e < V; ++e) acc[V * hb + e] = mfma_f32(x[e], s[y][i], acc[V * hb + e]);
                                 }
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < V; ++e) acc[V * hb + e] = mfma_f32(x[e], s[y][i], acc[V * hb + e]);
                             }
                         }
-                }
-                ++e;
-                return true;
-            });
-            const bool bad = non_finite<DB>(acc);
-            if (!__syncthreads_or(bad) || careful) break;
-            careful = true;
-        }
-
-        const float l_tot = sum_over_g(l_run);
-        if (row0 + r >= t.n) continue;
-        const bool none = no_key(l_tot);
-        const float inv = a.put_state ? 1.f : none ? 0.f : 1.f / l_tot;
-        if (a.put_state && row.i < a.shift) continue;
-        float* dst = a.put_state ? a.state_o + at_row * D : o + token * a.ot + h * a.oh;
-#pragma unroll
-        for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                vec x;
-#pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = acc[V * hb + e][i] * inv;
-                *reinterpret_cast<vec*>(dst + 16 * V * hb + V * (4 * g + i)) = x;
+                    }
             }
-        if (g != 0) continue;
-        if (a.put_state) {
-            a.state_ml[2 * at_row] = m_run;
-            a.state_ml[2 * at_row + 1] = l_tot;
-        } else {
-            a.lse[at_row] = none ? -INFINITY : (m_run * c2 + __log2f(l_tot)) / kLog2e;
+            ++e;
+            return true;
+        });
+        const bool bad = non_finite<DB>(acc);
+        if (!__syncthreads_or(bad) || careful) break;
+        careful = true;
+    }
+
+    const float l_tot = sum_over_g(l_run);
+    if (row0 + r >= t.n) return;
+    const bool none = no_key(l_tot);
+    const float inv = a.put_state ? 1.f : none ? 0.f : 1.f / l_tot;
+    if (a.put_state && row.i < a.shift) return;
+    float* dst = a.put_state ? a.state_o + at_row * D : o + token * a.ot + h * a.oh;
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vec x;
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = acc[V * hb + e][i] * inv;
+            *reinterpret_cast<vec*>(dst + 16 * V * hb + V * (4 * g + i)) = x;
         }
+    if (g != 0) return;
+    if (a.put_state) {
+        a.state_ml[2 * at_row] = m_run;
+        a.state_ml[2 * at_row + 1] = l_tot;
+    } else {
+        a.lse[at_row] = none ? -INFINITY : (m_run * c2 + __log2f(l_tot)) / kLog2e;
     }
 }
 
 // ---------------------------------------------------------------------------
 // Launches
 // ---------------------------------------------------------------------------
-constexpr int64_t kMaxGrid = 1 << 20;      // workgroups; each takes every kMaxGrid-th place
+constexpr int64_t kMaxGridX = 1 << 20;     // workgroups along x; along y the rest
 constexpr int64_t kWidePlaces = 1024;      // tiles of 128 rows from so many workgroups on
+
+dim3 grid_of(const PackedArgs& a) {
+    const int64_t n = a.places * a.run_heads;
+    return dim3((unsigned)min64(n, kMaxGridX), (unsigned)((n + kMaxGridX - 1) / kMaxGridX));
+}
 
 int64_t tile_places(const PackedArgs& a, int rows) {
     if (a.step == 1) return a.tokens / rows + a.sequences;
@@ -716,27 +796,24 @@ int64_t tile_places(const PackedArgs& a, int rows) {
     return min64((int64_t)a.step * (a.tokens / min64(per, 0x7fffffff) + a.sequences), a.tokens);
 }
 
-template <int D, bool WIDE, bool FIXED_>
+template <int D, int NW, bool FIXED_>
 hipError_t run_bf16(PackedArgs& a, const PackedCall& p, hipStream_t stream) {
-    constexpr int ROWS = PackedCfg<D, WIDE>::ROWS;
-    a.places = tile_places(a, ROWS);
+    a.places = tile_places(a, 32 * NW);
     a.by_rows = a.step > 1 && a.places == a.tokens;
-    const dim3 grid((unsigned)min64(a.places * a.run_heads, kMaxGrid));
-    hipLaunchKernelGGL((packed_bf16_kernel<D, WIDE, FIXED_>), grid, dim3(kPackedThreads), 0, stream, a,
-                       (const uint16_t*)p.q, (const uint16_t*)p.k, (const uint16_t*)p.v, (uint16_t*)p.o);
+    hipLaunchKernelGGL((packed_bf16_kernel<D, NW, FIXED_>), grid_of(a), dim3(64 * NW), 0, stream, a, (const uint16_t*)p.q,
+                       (const uint16_t*)p.k, (const uint16_t*)p.v, (uint16_t*)p.o);
     return hipGetLastError();
 }
 
 template <int D, bool FIXED_>
 hipError_t run(PackedArgs& a, const PackedCall& p, hipStream_t stream) {
     if (p.dtype == 1) {
-        if (tile_places(a, PackedCfg<D, true>::ROWS) * a.run_heads >= kWidePlaces) return run_bf16<D, true, FIXED_>(a, p, stream);
-        return run_bf16<D, false, FIXED_>(a, p, stream);
+        if (D == 128 || tile_places(a, 128) * a.run_heads >= kWidePlaces) return run_bf16<D, 4, FIXED_>(a, p, stream);
+        if constexpr (D < 128) return run_bf16<D, 2, FIXED_>(a, p, stream);
     }
     a.places = tile_places(a, 16 * kPackedWaves);
     a.by_rows = a.step > 1 && a.places == a.tokens;
-    const dim3 grid((unsigned)min64(a.places * a.run_heads, kMaxGrid));
-    hipLaunchKernelGGL((packed_f32_kernel<D, FIXED_>), grid, dim3(kPackedThreads), 0, stream, a, (const float*)p.q,
+    hipLaunchKernelGGL((packed_f32_kernel<D, FIXED_>), grid_of(a), dim3(kPackedThreads), 0, stream, a, (const float*)p.q,
                        (const float*)p.k, (const float*)p.v, (float*)p.o);
     return hipGetLastError();
 }
