@@ -920,7 +920,7 @@ int sparse_attn_paged_decode_workspace_size(int64_t max_pos, int32_t stride_l, i
     if (kv_heads < 1 || heads % kv_heads != 0 || !bytes) return SA_ERR_INVALID;
     if ((int64_t)batch * heads >= kMaxRows8) return SA_ERR_UNSUPPORTED;
     *bytes = sa::paged_decode_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c, batch,
-                                              heads, kv_heads, d_head, dtype);
+                                              heads, kv_heads, d_head);
     return SA_OK;
 }
 
@@ -950,7 +950,7 @@ int sparse_attn_paged_decode(const int32_t* positions, int64_t max_pos, int32_t 
     if (!rows_apart(o_strides, batch, heads, d_head)) return SA_ERR_INVALID;
     if (!isfinite(softmax_scale) || !(softmax_scale > 0.f)) return SA_ERR_INVALID;
     const size_t need = sa::paged_decode_workspace_bytes(internal, head_mode, sub, (int32_t)max_pos, stride_l, summary_c,
-                                                         batch, heads, kv_heads, d_head, dtype);
+                                                         batch, heads, kv_heads, d_head);
     if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
     if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
     p.table = table;

@@ -43,6 +43,12 @@ struct Decode8Args {
     DivL dc;
     int64_t qsb, qsh, osb, osh;  // strides of q and o
     float scale_log2;
+    // Ranges of a row, and where their states lie.
+    __device__ int ranges(int64_t b, int64_t h, int64_t* first, int64_t* step) const {
+        *first = (b * heads + h) * splits;
+        *step = 1;
+        return splits;
+    }
 };
 
 // Eight elements of a query as bf16 pieces that sum to them: one of bf16, three of fp32.
@@ -342,7 +348,7 @@ hipError_t launch(const Decode8Args& a, int batch, const void* q, void* o, float
     }
     hipLaunchKernelGGL((decode8_split_kernel<D, T, kWaves, false>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o,
                        lse);
-    return step_combine<D, T>(a, batch, part, o, lse, stream);
+    return step_combine<D, T>(a, batch, a.splits, part, o, lse, stream);
 }
 
 // Ranges per unit, for the largest set that a position up to max_pos can have.

@@ -394,7 +394,7 @@ struct PagedStep {
     int32_t pages, shift;
 };
 size_t paged_decode_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c,
-                                    int batch, int heads, int kv_heads, int d, int dtype);
+                                    int batch, int heads, int kv_heads, int d);
 hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l,
                                int32_t c, int batch, int heads, int kv_heads, int d, int dtype, const void* q,
                                const int64_t* q_strides, float scale, void* o, const int64_t* o_strides, float* lse,

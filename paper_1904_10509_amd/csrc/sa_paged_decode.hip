@@ -37,10 +37,93 @@ struct PagedArgs {
     int pattern, mode, heads, kv_heads, splits;
     HeadUnits u;
     int32_t sub, max_pos, l, sc;
+    int32_t least;               // keys of a range, at least
+    int32_t batch;
+    int2* cuts;                  // [batch, heads]: first range and ranges of a row
     DivL dc;
     int64_t qsb, qsh, osb, osh;  // strides of q and o
     float scale_log2;
+
+    // The set of head h at a position.
+    __device__ DecodeSet set(int h, int32_t pos) const {
+        return DecodeSet(pattern, part_of_head(mode, h), pos, l, sc, (int32_t)summary_start(l, sc, subblock_of_head(sub, h)),
+                         dc);
+    }
+    // Ranges of a row, and where their states lie: range i of the batch has one for each head.
+    __device__ int ranges(int64_t b, int64_t h, int64_t* first, int64_t* step) const;
 };
+
+// How the sets of a batch are cut for one head: every sequence into equal ranges of at most `per` keys, all of
+// them about `target` (PagedArgs::splits) ranges together, numbered through the batch.  Sequences of different
+// lengths then take as long as each other: a fixed number of ranges for each, 16 sequences between 866 and 32,767
+// keys (4 cache heads of 128, 8 query heads each) took 93.2 us, this way XX.  Every wave makes the sums by itself, a
+// sequence a lane.
+struct Share {
+    int64_t b;        // the sequence of a range (-1: there is none)
+    int32_t base;     // ranges of the sequences before it
+    int32_t ranges;   // its own
+    uint32_t count;   // keys of its set
+};
+__device__ inline uint32_t keys_of(const PagedArgs& a, int h, int64_t b) {
+    const int32_t pos = b < a.batch ? a.positions[b] : -1;
+    return pos >= 0 && pos <= a.max_pos ? (uint32_t)a.set(h, pos).count : 0u;
+}
+// Sum over the lanes up to this one: within rows of 16 lanes, then across them, in registers.
+__device__ inline int32_t sum_upto(int32_t x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31 into rows 2 and 3
+    return x;
+}
+__device__ inline Share share_of(const PagedArgs& a, int h, int32_t range, int lane) {
+    // in pieces of 64 keys, rounded up: 64 sequences' are within 31 bits
+    const uint32_t mine = keys_of(a, h, lane);  // the first 64 sequences: read once
+    uint64_t total = 0;
+    for (int64_t b0 = 0; b0 < a.batch; b0 += 64) {
+        const uint32_t count = b0 == 0 ? mine : keys_of(a, h, b0 + lane);
+        total += (uint32_t)__builtin_amdgcn_readlane(sum_upto((int32_t)((count >> 6) + (count % 64 != 0))), 63);
+    }
+    const uint32_t pieces = total >> 31 == 0 ? ((uint32_t)total + a.splits - 1) / a.splits
+                                             : (uint32_t)min((total + a.splits - 1) / a.splits, (uint64_t)1 << 25);
+    uint32_t per = max(pieces << 6, (uint32_t)a.least);
+    if (a.batch <= 64) {
+        // rounded up for each sequence, they can be more than `splits`: longer ones, until they are not
+        for (int i = 0; i < 3; ++i) {
+            const int32_t n = __builtin_amdgcn_readlane(sum_upto(mine == 0 ? 0 : (int32_t)((mine - 1) / per + 1)), 63);
+            if (n <= a.splits) break;
+            per = (uint32_t)min64(((int64_t)per * n / a.splits + 64) & ~63ll, (int64_t)1 << 31);
+        }
+    }
+    Share s{-1, 0, 0, 0};
+    for (int64_t b0 = 0; b0 < a.batch; b0 += 64) {
+        const uint32_t count = b0 == 0 ? mine : keys_of(a, h, b0 + lane);
+        const int32_t n = count == 0 ? 0 : (int32_t)((count - 1) / per + 1);
+        const int32_t end = s.base + sum_upto(n);  // ranges up to this sequence
+        const uint64_t up = __builtin_amdgcn_ballot_w64(end > range);
+        if (up) {
+            const int at = __builtin_ctzll(up);
+            s.b = b0 + at;
+            s.ranges = __builtin_amdgcn_readlane(n, at);
+            s.base = __builtin_amdgcn_readlane(end, at) - s.ranges;
+            s.count = (uint32_t)__builtin_amdgcn_readlane((int)count, at);
+            return s;
+        }
+        s.base = __builtin_amdgcn_readlane(end, 63);
+    }
+    return s;
+}
+// The row's first range leaves both numbers for the join; a row without a key has none.
+__device__ inline int PagedArgs::ranges(int64_t b, int64_t h, int64_t* first, int64_t* step) const {
+    *step = heads;
+    *first = 0;
+    if (keys_of(*this, (int)h, b) == 0) return 0;
+    const int2 at = cuts[b * heads + h];
+    *first = (int64_t)at.x * heads + h;
+    return at.y;
+}
 
 __device__ inline f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -181,22 +264,30 @@ paged_split_kernel(PagedArgs a, const T* __restrict__ q, float* __restrict__ par
 
     const int tid = threadIdx.x, lane = tid % 64, w = __builtin_amdgcn_readfirstlane(tid / 64);
     const int g = lane / 16, r = lane % 16;
-    const uint32_t per_split = gridDim.x / a.splits;
-    const int split = (int)(blockIdx.x / per_split);
-    const uint32_t id = blockIdx.x % per_split;
-    const int unit = (int)(id % a.u.units);
-    const int64_t b = id / a.u.units;
+    const int unit = (int)(blockIdx.x % a.u.units);
     const int tile = unit % a.u.tiles, cls = unit / a.u.tiles % a.u.classes, kvh = unit / (a.u.tiles * a.u.classes);
     const int h0 = kvh * a.u.group + cls + tile * kCols * a.u.period;  // column c is head h0 + c * period
     const int left = (kvh + 1) * a.u.group - h0;
     const int cols = min(kCols, (left + a.u.period - 1) / a.u.period);  // < 1 for a class that has no such tile
-
+    if (cols < 1) return;
+    // the sequence and its keys t0 .. t1 - 1: all of them (one range a sequence), or the range of this workgroup
+    int64_t b = blockIdx.x / a.u.units;
+    const int32_t range = (int32_t)b;
+    uint32_t t0 = 0, t1;
+    if constexpr (DIRECT) {
+        t1 = keys_of(a, h0, b);
+    } else {
+        const Share s = share_of(a, h0, range, lane);
+        if (s.b < 0) return;
+        b = s.b;
+        // equal ranges of the sequence
+        const uint32_t per = (s.count + s.ranges - 1) / s.ranges;
+        t0 = min((range - s.base) * per, s.count);
+        if (range == s.base && tid < cols) a.cuts[b * a.heads + h0 + tid * a.u.period] = make_int2(s.base, s.ranges);
+        t1 = min(t0 + per, s.count);
+    }
     const int32_t pos = a.positions[b];
-    const bool live = pos >= 0 && pos <= a.max_pos && cols > 0;
-    const KeySet set(DecodeSet(a.pattern, part_of_head(a.mode, h0), live ? pos : 0, a.l, a.sc,
-                               (int32_t)summary_start(a.l, a.sc, subblock_of_head(a.sub, h0)), a.dc));
-    const uint32_t count = live ? set.count : 0, per = (count + a.splits - 1) / a.splits;
-    const uint32_t t0 = min(split * per, count), t1 = min(t0 + per, count);
+    const KeySet set(a.set(h0, max(0, min(pos, a.max_pos))));
 
     WaveLds<D, T>& mine = lds.wave[w];
     // this lane's piece: of row 64 / PR * i + lane / PR in load i
@@ -355,7 +446,7 @@ paged_split_kernel(PagedArgs a, const T* __restrict__ q, float* __restrict__ par
                 else lse[row] = no_key(total) ? -INFINITY : (s_top[c] * a.scale_log2 + __log2f(total)) / kLog2e;
             }
         } else {
-            float* dst = part + (row * a.splits + split) * (D + 2);
+            float* dst = part + ((int64_t)range * a.heads + head) * (D + 2);
             dst[e] = sum;
             if (e == 0) {
                 dst[D] = s_top[c];
@@ -366,37 +457,39 @@ paged_split_kernel(PagedArgs a, const T* __restrict__ q, float* __restrict__ par
 }
 
 template <int D, typename T>
-hipError_t launch(const PagedArgs& a, int batch, const void* q, void* o, float* lse, float* part, hipStream_t stream) {
-    const dim3 grid((unsigned)((int64_t)batch * a.u.units * a.splits)), wg(kWaves * 64);
-    if (a.splits == 1) {
-        hipLaunchKernelGGL((paged_split_kernel<D, T, true>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o, lse);
+hipError_t launch(const PagedArgs& a, const void* q, void* o, float* lse, float* part, hipStream_t stream) {
+    const dim3 wg(kWaves * 64);
+    if (a.splits == 0) {
+        hipLaunchKernelGGL((paged_split_kernel<D, T, true>), dim3((unsigned)((int64_t)a.batch * a.u.units)), wg, 0, stream, a,
+                           (const T*)q, part, (T*)o, lse);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((paged_split_kernel<D, T, false>), grid, wg, 0, stream, a, (const T*)q, part, (T*)o, lse);
-    return step_combine<D, T>(a, batch, part, o, lse, stream);
+    hipLaunchKernelGGL((paged_split_kernel<D, T, false>), dim3((unsigned)((int64_t)(a.splits + a.batch) * a.u.units)), wg, 0,
+                       stream, a, (const T*)q, part, (T*)o, lse);
+    return step_combine<D, T>(a, a.batch, 2 * a.splits / a.batch, part, o, lse, stream);
 }
 
-// Ranges per unit, for the largest set that a position up to max_pos can have.
-int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t units, int64_t rows,
-              int d) {
+// Ranges that a call's sets are cut into (about; one more for each sequence at most), 0 where every sequence is one.
+//   One up to 256 keys: there is nothing to join.
+//   Else as many as fill the workgroups that run at once (2 a compute unit for d = 128, whose rows take 68 KB of
+//   LDS, 3 for d = 64, 5 for d = 32), so that they end together;
+//   with more sequences than that allows, four for each: short ranges even out over several rounds.
+// No range has fewer than 128 keys, one chunk a wave (two of fp32).
+constexpr int32_t kLeastKeys = 128;
+int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t batch, int64_t units, int d) {
     const int64_t count = largest_set(pattern, mode, sub, max_pos, l, c);
-    if (count <= 256) return 1;
-    const int64_t finest = (count + 127) / 128, target = d == 128 ? 512 : 1024;
-    const int64_t few = max64(min64(units * finest * 4 <= target * 5 ? finest : target / units, 128), 1);
-    if (count <= 2048 * few) return (int)few;
-    int64_t many = min64(min64(count / (d == 128 ? 1024 : 512), 4096 / rows), 512);
-    const int64_t rounds = units * many / 1024;
-    if (rounds > 0) many = rounds * 1024 / units;
-    return (int)max64(few, many);
+    if (count <= 256) return 0;
+    const int64_t places = 256 * (d == 128 ? 2 : d == 64 ? 3 : 5) / units;  // of one unit
+    const int64_t n = places >= 2 * batch ? places : 4 * batch;
+    return (int)max64(1, min64(n, batch * ((count + kLeastKeys - 1) / kLeastKeys)));
 }
 
 }  // namespace
 
 size_t paged_decode_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c,
-                                    int batch, int heads, int kv_heads, int d, int dtype) {
-    const int64_t units = (int64_t)batch * head_units(mode, sub, heads, kv_heads).units;
-    const int64_t rows = (int64_t)batch * heads;
-    return (size_t)rows * splits_of(pattern, mode, sub, max_pos, l, c, units, rows, d) * (d + 2) * sizeof(float);
+                                    int batch, int heads, int kv_heads, int d) {
+    const int splits = splits_of(pattern, mode, sub, max_pos, l, c, batch, head_units(mode, sub, heads, kv_heads).units, d);
+    return splits == 0 ? 0 : (size_t)(splits + batch) * heads * (d + 2) * sizeof(float) + (size_t)batch * heads * sizeof(int2);
 }
 
 hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l,
@@ -415,7 +508,9 @@ hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_
     a.heads = heads;
     a.kv_heads = kv_heads;
     a.u = head_units(mode, sub, heads, kv_heads);
-    a.splits = splits_of(pattern, mode, sub, max_pos, l, c, (int64_t)batch * a.u.units, (int64_t)batch * heads, d);
+    a.batch = batch;
+    a.splits = splits_of(pattern, mode, sub, max_pos, l, c, batch, a.u.units, d);
+    a.least = kLeastKeys;
     a.sub = sub;
     a.max_pos = max_pos;
     a.l = l;
@@ -427,17 +522,18 @@ hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_
     a.osh = o_strides[1];
     a.scale_log2 = scale * kLog2eHost;
     float* part = static_cast<float*>(workspace);
+    a.cuts = reinterpret_cast<int2*>(part + (int64_t)(a.splits + batch) * heads * (d + 2));  // (d + 2 is even)
     if (dtype == 1) {
         switch (d) {
-        case 32: return launch<32, uint16_t>(a, batch, q, o, lse, part, stream);
-        case 64: return launch<64, uint16_t>(a, batch, q, o, lse, part, stream);
-        default: return launch<128, uint16_t>(a, batch, q, o, lse, part, stream);
+        case 32: return launch<32, uint16_t>(a, q, o, lse, part, stream);
+        case 64: return launch<64, uint16_t>(a, q, o, lse, part, stream);
+        default: return launch<128, uint16_t>(a, q, o, lse, part, stream);
         }
     }
     switch (d) {
-    case 32: return launch<32, float>(a, batch, q, o, lse, part, stream);
-    case 64: return launch<64, float>(a, batch, q, o, lse, part, stream);
-    default: return launch<128, float>(a, batch, q, o, lse, part, stream);
+    case 32: return launch<32, float>(a, q, o, lse, part, stream);
+    case 64: return launch<64, float>(a, q, o, lse, part, stream);
+    default: return launch<128, float>(a, q, o, lse, part, stream);
     }
 }
 

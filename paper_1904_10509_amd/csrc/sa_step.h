@@ -83,14 +83,16 @@ step_combine_kernel(Args a, const float* __restrict__ part, T* __restrict__ o, f
     __shared__ float s_x[G][D], s_l[G], s_m[G];
     const int64_t row = blockIdx.x, b = row / a.heads, h = row % a.heads;
     const int tid = threadIdx.x, g = tid / D, e = tid % D;
-    const float* src = part + row * a.splits * (D + 2);
+    int64_t first, step;  // the row's states: the first one, and from one to the next
+    const int splits = a.ranges(b, h, &first, &step);
+    const float* src = part + first * (D + 2);
     float m = -INFINITY, l = 0.f, x = 0.f;
-    for (int s0 = g; s0 < a.splits; s0 += U * G) {
+    for (int s0 = g; s0 < splits; s0 += U * G) {
         float ms[U], ls[U], xs[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + u * G;
-            const float* p = src + (int64_t)(s < a.splits ? s : s0) * (D + 2);
+            const float* p = src + (s < splits ? s : s0) * step * (D + 2);
             xs[u] = p[e];
             ms[u] = p[D];
             ls[u] = p[D + 1];
@@ -104,7 +106,7 @@ step_combine_kernel(Args a, const float* __restrict__ part, T* __restrict__ o, f
         m = mx;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float wt = s0 + u * G < a.splits ? weight(ms[u], mx, a.scale_log2) : 0.f;
+            const float wt = s0 + u * G < splits ? weight(ms[u], mx, a.scale_log2) : 0.f;
             l = fmaf(ls[u], wt, l);
             x = fmaf(xs[u], wt, x);
         }
@@ -137,12 +139,12 @@ step_combine_kernel(Args a, const float* __restrict__ part, T* __restrict__ o, f
     }
 }
 
-// One thread for each of a row's D elements and up to 16 ranges; more ranges, four times the threads (4
-// sequences of 8 cache heads of 64, 18 ranges of an 8-bit cache: 9.8 -> 9.1 us).
+// One thread for each of a row's D elements and up to 16 ranges (`most` of a row, about); more ranges, four times
+// the threads (4 sequences of 8 cache heads of 64, 18 ranges of an 8-bit cache: 9.8 -> 9.1 us).
 template <int D, typename T, typename Args>
-hipError_t step_combine(const Args& a, int batch, const float* part, void* o, float* lse, hipStream_t stream) {
+hipError_t step_combine(const Args& a, int batch, int most, const float* part, void* o, float* lse, hipStream_t stream) {
     const dim3 rows((unsigned)(batch * a.heads));
-    if (a.splits > 16)
+    if (most > 16)
         hipLaunchKernelGGL((step_combine_kernel<D, T, 1024, Args>), rows, dim3(1024), 0, stream, a, part, (T*)o, lse);
     else
         hipLaunchKernelGGL((step_combine_kernel<D, T, 256, Args>), rows, dim3(256), 0, stream, a, part, (T*)o, lse);

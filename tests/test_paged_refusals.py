@@ -55,20 +55,20 @@ def test_paged_store_refusals(L, over, expect):
     assert L.sparse_attn_paged_store(*dict(STORE, **over).values()) == expect
 
 
-DECODE = dict(positions=FAKE, max_pos=600, l=128, c=32, pattern=sa.SA_FIXED, mode=sa.SA_MODE_MERGED, batch=2, heads=8, kv=4,
+DECODE = dict(positions=FAKE, max_pos=6000, l=128, c=32, pattern=sa.SA_FIXED, mode=sa.SA_MODE_MERGED, batch=2, heads=8, kv=4,
               d=64, dtype=sa.SA_BF16, q=FAKE, qs=longs(512, 64), kp=FAKE, vp=FAKE + 128, ps=longs(32768, 8192, 128), pages=30,
-              page=64, table=FAKE, ts=10, max_pages=10, scale=0.125, o=FAKE, os=longs(512, 64), lse=FAKE, ws=FAKE,
+              page=64, table=FAKE, ts=100, max_pages=100, scale=0.125, o=FAKE, os=longs(512, 64), lse=FAKE, ws=FAKE,
               nbytes=1 << 30, stream=None)
 
 
 @pytest.mark.parametrize("over,expect", [
-    (dict(positions=None), INV), (dict(positions=FAKE + 1), INV), (dict(max_pos=-1), INV), (dict(max_pos=640), INV),
+    (dict(positions=None), INV), (dict(positions=FAKE + 1), INV), (dict(max_pos=-1), INV), (dict(max_pos=6400), INV),
     (dict(max_pos=2 ** 31), INV), (dict(l=0), INV), (dict(c=0), INV), (dict(c=129), INV), (dict(pattern=3), INV),
     (dict(mode=4), INV), (dict(pattern=sa.SA_FIXED_PER_HEAD, c=1), UNS), (dict(batch=0), INV), (dict(heads=0), INV),
     (dict(kv=3), INV), (dict(kv=0), INV), (dict(batch=2 ** 20), UNS), (dict(d=96), UNS), (dict(dtype=5), INV),
     (dict(q=None), INV), (dict(q=FAKE + 2), INV), (dict(qs=longs(512, 60)), INV), (dict(kp=None), INV), (dict(ps=None), INV),
     (dict(ps=longs(32768, 8192, 32)), INV), (dict(pages=0), INV), (dict(pages=2 ** 30), UNS), (dict(page=24), INV),
-    (dict(table=None), INV), (dict(table=FAKE + 2), INV), (dict(ts=9), INV), (dict(ts=-1), INV), (dict(max_pages=0), INV),
+    (dict(table=None), INV), (dict(table=FAKE + 2), INV), (dict(ts=99), INV), (dict(ts=-1), INV), (dict(max_pages=0), INV),
     (dict(scale=0.0), INV), (dict(scale=float("nan")), INV), (dict(scale=float("inf")), INV), (dict(o=None), INV),
     (dict(os=longs(512, 0)), INV), (dict(os=longs(0, 64)), INV), (dict(lse=None), INV), (dict(lse=FAKE + 2), INV),
     (dict(ws=None), INV), (dict(ws=FAKE + 8), INV), (dict(nbytes=0), SMALL),
@@ -78,10 +78,11 @@ def test_paged_decode_refusals(L, over, expect):
 
 
 def test_paged_decode_workspace(L):
-    args = dict(max_pos=600, l=128, c=32, pattern=sa.SA_FIXED, mode=sa.SA_MODE_MERGED, batch=2, heads=8, kv=4, d=64,
+    args = dict(max_pos=6000, l=128, c=32, pattern=sa.SA_FIXED, mode=sa.SA_MODE_MERGED, batch=2, heads=8, kv=4, d=64,
                 dtype=sa.SA_BF16)
     need = sa.sparse_attn_paged_decode_workspace_size(*args.values())
-    assert need > 0 and need % (2 * 8 * 66 * 4) == 0
+    assert need > 0 and (need - 2 * 8 * 8) % (8 * 66 * 4) == 0  # a state of each head for every range
+    assert sa.sparse_attn_paged_decode_workspace_size(*dict(args, max_pos=255).values()) == 0  # one range a sequence
     out = ctypes.c_size_t()
     for over, expect in ((dict(kv=5), INV), (dict(max_pos=-1), INV), (dict(d=16), UNS), (dict(batch=2 ** 20), UNS),
                          (dict(dtype=9), INV)):
