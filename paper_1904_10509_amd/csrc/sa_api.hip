@@ -995,11 +995,12 @@ int sparse_attn_packed_fwd(int32_t sequences, const int32_t* starts, int64_t tok
         if (!rows_ok(strides, 2, unit, 0)) return SA_ERR_INVALID;
     if (!rows_apart(o_strides, tokens > 1 ? 2 : 1, heads, d_head)) return SA_ERR_INVALID;
     if (!isfinite(softmax_scale) || !(softmax_scale > 0.f)) return SA_ERR_INVALID;
+    p.sequences = sequences;
+    if (!sa::packed_fits(p)) return SA_ERR_UNSUPPORTED;
     const size_t need = sa::packed_workspace_bytes(tokens, p.pattern, head_mode, stride_l, heads, d_head);
     if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
     if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
     p.starts = starts;
-    p.sequences = sequences;
     p.q = q, p.k = k, p.v = v, p.o = o;
     p.qt = q_strides[0], p.qh = q_strides[1];
     p.kt = k_strides[0], p.kh = k_strides[1];

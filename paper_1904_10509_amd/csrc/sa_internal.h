@@ -415,6 +415,7 @@ struct PackedCall {
     float* workspace;
 };
 size_t packed_workspace_bytes(int64_t tokens, int32_t pattern, int32_t mode, int32_t l, int32_t heads, int32_t d);
+bool packed_fits(const PackedCall& c);  // whether its launches number their workgroups in 31 bits
 hipError_t packed_launch(const PackedCall& c, hipStream_t stream);
 
 size_t bwd_workspace_bytes(int64_t batch, int64_t heads, int64_t n, int64_t nq, int n_layouts);

@@ -55,80 +55,83 @@ struct PackedArgs {
 };
 
 // Tile of a place: rows i0, i0 + 1, ... (counted in steps) below n of the sequence (or class) whose first
-// row is `base`.
+// row is `base`.  n = 0: an empty place.
 struct TilePlace {
     int32_t base, n, i0;
-    int32_t offset;  // of the first row in its sequence
 };
 
-// Every wave finds its sequence by itself: 64 candidates a round, all loads of a round at once.
-__device__ inline int sequence_of(const PackedArgs& a, int rows, int64_t place, int lane) {
-    int found = 0;
+// Every wave finds the sequence of a place by itself: 64 candidates a round, all loads of a round at once.
+struct Found {
+    int32_t s, start, end;  // s < 0: none
+};
+__device__ inline Found sequence_of(const PackedArgs& a, uint32_t rows, uint32_t place, int lane) {
+    Found f{-1, 0, 0};
     for (int s0 = 0; s0 < a.sequences; s0 += 64) {
         const int s = s0 + lane;
+        int32_t start = 0, end = 0;
         bool below = false;
         if (s < a.sequences) {
-            const int32_t start = max(0, min(a.starts[s], a.tokens));
-            below = a.by_rows ? start <= place : (int64_t)(start / rows) + s <= place;
+            start = max(0, min(a.starts[s], a.tokens));
+            end = max(0, min(a.starts[s + 1], a.tokens));
+            below = a.by_rows ? (uint32_t)start <= place : (uint32_t)start / rows + s <= place;
         }
         const uint64_t m = __builtin_amdgcn_ballot_w64(below);
-        found += __builtin_popcountll(m);
+        const int found = __builtin_popcountll(m);  // (places begin in the order of the sequences)
+        if (found > 0) {
+            f.s = s0 + found - 1;
+            f.start = __builtin_amdgcn_readlane(start, found - 1);
+            f.end = __builtin_amdgcn_readlane(end, found - 1);
+        }
         if (~m) break;
     }
-    return found - 1;  // (the first sequence's places begin at its start; found = 0 lies before it)
+    return f;
 }
 
 template <int ROWS>
-__device__ inline TilePlace tile_place(const PackedArgs& a, int64_t place, int lane) {
-    int32_t cls = 0;
-    const int64_t rows = (int64_t)ROWS * a.step;
+__device__ inline TilePlace tile_place(const PackedArgs& a, uint32_t place, int lane) {
+    uint32_t cls = 0;
     if (a.step > 1 && !a.by_rows) {
-        const int64_t block = place / a.l;
-        cls = (int32_t)(place - block * a.l);
+        const uint32_t block = place / (uint32_t)a.l;
+        cls = place - block * a.l;
         place = block;
     }
-    const int32_t per = (int32_t)min64(rows, 0x7fffffff);
-    const int s = __builtin_amdgcn_readfirstlane(sequence_of(a, per, place, lane));
-    if (s < 0) return {0, 0, 0, 0};
-    const int32_t start = __builtin_amdgcn_readfirstlane(max(0, min(a.starts[s], a.tokens)));
-    const int32_t end = __builtin_amdgcn_readfirstlane(max(0, min(a.starts[s + 1], a.tokens)));
-    const int32_t n = end - start;
-    int64_t tile;
+    const uint32_t per = (uint32_t)min64((int64_t)ROWS * a.step, 0x7fffffff);
+    const Found f = sequence_of(a, per, place, lane);
+    const int32_t n = f.end - f.start;
+    if (f.s < 0 || n <= 0) return {0, 0, 0};
+    uint32_t tile;
     if (a.by_rows) {
-        const int64_t i = place - start;
-        if (i >= n) return {0, 0, 0, 0};
-        const int32_t m = div_l(a.dl, (int32_t)i);
-        if (m % ROWS != 0) return {0, 0, 0, 0};
-        cls = (int32_t)i - m * a.l;
+        const uint32_t i = place - f.start;
+        if (i >= (uint32_t)n) return {0, 0, 0};
+        const uint32_t m = (uint32_t)div_l(a.dl, (int32_t)i);
+        if (m % ROWS != 0) return {0, 0, 0};
+        cls = i - m * a.l;
         tile = m / ROWS;
     } else {
-        tile = place - ((int64_t)(start / per) + s);
+        tile = place - ((uint32_t)f.start / per + f.s);
     }
-    if (n <= cls || tile < 0) return {0, 0, 0, 0};
-    const int32_t rows_here = a.step == 1 ? n : div_l(a.dl, n - 1 - cls) + 1;
-    const int64_t i0 = tile * ROWS;
-    if (i0 >= rows_here) return {0, 0, 0, 0};
-    return {start + cls, rows_here, (int32_t)i0, cls};
+    if ((uint32_t)n <= cls) return {0, 0, 0};
+    const int32_t rows = a.step == 1 ? n : div_l(a.dl, n - 1 - (int32_t)cls) + 1;
+    if (tile > (uint32_t)(rows - 1) / ROWS) return {0, 0, 0};
+    return {f.start + (int32_t)cls, rows, (int32_t)(tile * ROWS)};
 }
 
 // Consecutive workgroups go to the 8 XCDs in turn: with heads in eighths, an XCD takes neighbouring heads, which
 // share key heads, and their keys stay in its L2.  Places from the last one down: a sequence's longest walks first.
-__device__ inline bool place_of(const PackedArgs& a, int64_t* place, int* head) {
-    const int64_t id = blockIdx.x + (int64_t)gridDim.x * blockIdx.y;
-    if (id >= a.places * a.run_heads) return false;
-    int h;
-    int64_t p;
-    if (a.run_heads % 8 == 0) {
-        const int each = a.run_heads / 8;
-        const int64_t s = id / 8;
-        p = s / each;
-        h = (int)(id % 8) * each + (int)(s - p * each);
+__device__ inline bool place_of(const PackedArgs& a, uint32_t* place, int* head) {
+    const uint32_t id = blockIdx.x + gridDim.x * blockIdx.y, run = (uint32_t)a.run_heads;
+    if (id >= (uint32_t)a.places * run) return false;
+    uint32_t p, h;
+    if (run % 8 == 0) {
+        const uint32_t each = run / 8;
+        p = id / 8 / each;
+        h = id % 8 * each + (id / 8 - p * each);
     } else {
-        p = id / a.run_heads;
-        h = (int)(id - p * a.run_heads);
+        p = id / run;
+        h = id - p * run;
     }
-    *place = a.places - 1 - p;
-    *head = a.head0 + h * a.head_step;
+    *place = (uint32_t)a.places - 1 - p;
+    *head = a.head0 + (int)h * a.head_step;
     return true;
 }
 
@@ -275,10 +278,10 @@ __device__ inline void accumulate_bits(const bf16x8* a, bf16x8 b, uint32_t bits,
 }
 
 template <int D, int NW, bool FIXED_>
-__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 3)))
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(D == 128 || (D == 64 && NW == 2) ? 2 : 3)))
 packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
                    const uint16_t* __restrict__ v, uint16_t* __restrict__ o) {
-    constexpr int KEYS = 64, ROWS = 32 * NW, KS = D / 16, DB = D / 32;
+    constexpr int KEYS = 64, ROWS = 32 * NW, KS = D / 16, DB = D / 32, PRE = D == 128 ? 8 : 2 * KS;
     __shared__ __attribute__((aligned(16))) uint16_t sK[2][KEYS * D];
     __shared__ __attribute__((aligned(16))) uint16_t sV[2][KEYS * D];
     constexpr uint32_t kTileBytes = KEYS * D * 2;
@@ -301,7 +304,7 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
     static_assert(PER >= 1 && (NW * WR) % 16 == 0, "windows of a wave");
     const int wrow = lane / (64 / WR), chunk = (lane % (64 / WR)) ^ Swz<D>::perm(w * WR + wrow);
 
-    int64_t place;
+    uint32_t place;
     int h;
     if (!place_of(a, &place, &h)) return;
     const TilePlace t = tile_place<ROWS>(a, place, lane);
@@ -324,11 +327,6 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
     bf16x8 qf[KS];
     f32x16 acc[DB];
     float m_run, l_run;
-    {
-        const uint16_t* p = q + token * a.qt + h * a.qh;
-#pragma unroll
-        for (int x = 0; x < KS; ++x) qf[x] = ld_bf16x8(p + 16 * x + 8 * hh);
-    }
     // the state that the rows begin with: nothing, or what the classes left
     auto begin = [&] {
         m_run = -INFINITY;
@@ -348,24 +346,37 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
                 }
         }
     };
-    // one step's K and V rows to a ring stage.  Where a window's rows follow each other and exist, its address
-    // is one scalar; else every lane forms its row's.
-    const bool near_offsets = 32 * max64(ks, vs) < (int64_t)1 << 31;
-    const bool far_runs = FIXED_ && a.c % WR == 0;
-    const uint32_t k_off = (uint32_t)((wrow * ks + 8 * chunk) * 2), v_off = (uint32_t)((wrow * vs + 8 * chunk) * 2);
+    // One step's K and V rows to a ring stage.  Steps whose rows lie at the same distances from their first one (keys
+    // one behind the other; columns in runs of c that divide 64) take their addresses from a scalar that moves on by a
+    // constant; in the others, and where rows would lie behind the sequence, every lane forms its row's.
+    const bool even = ks == vs && 64 * ks < (int64_t)1 << 30;
+    const bool even_far = FIXED_ && even && KEYS % a.c == 0 && (KEYS / a.c) * (int64_t)a.l * ks < (int64_t)1 << 30;
+    uint32_t off[PER];
+    const uint16_t *kp = kh, *vp = vh;
+    int64_t forward = 0;
     auto load_step = [&](int e, int stage) {
         const bool far = FIXED_ && e < walk.far_steps;
         const int32_t first = far ? KEYS * e : walk.lo + KEYS * (e - walk.far_steps);
-        const bool whole = near_offsets && (far ? far_runs && first + KEYS <= walk.far : first + KEYS <= t.n);
+        if (e == 0 || (FIXED_ && e == walk.far_steps)) {
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                const int at = WR * (w + NW * x) + wrow;
+                const int32_t rows = far ? at / a.c * a.l + at % a.c : at;
+                off[x] = (uint32_t)((rows * ks + 8 * chunk) * 2);
+            }
+            const int64_t j = far ? win : walk.lo;
+            forward = (far ? (int64_t)(KEYS / a.c) * a.l : KEYS) * ks;
+            kp = kh + j * ks;
+            vp = vh + j * vs;
+        }
         const uint32_t kdst = sK_base + stage * kTileBytes, vdst = sV_base + stage * kTileBytes;
-        if (whole) {
+        if (far ? even_far && first + KEYS <= walk.far : even && first + KEYS <= t.n) {
+            const void *kb = uniform_ptr(kp), *vb = uniform_ptr(vp);
 #pragma unroll
             for (int x = 0; x < PER; ++x) {
                 const int window = w + NW * x;
-                const int64_t j = __builtin_amdgcn_readfirstlane(
-                    far ? key_row<FIXED_, KEYS>(a, win, walk, e, WR * window) : first + WR * window);
-                dma_b128(uniform_ptr(kh + j * ks), k_off, kdst + 1024 * window);
-                dma_b128(uniform_ptr(vh + j * vs), v_off, vdst + 1024 * window);
+                dma_b128(kb, off[x], kdst + 1024 * window);
+                dma_b128(vb, off[x], vdst + 1024 * window);
             }
         } else {
 #pragma unroll
@@ -376,6 +387,8 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
                 dma_b128_at(vh + j * vs + 8 * chunk, vdst + 1024 * window);
             }
         }
+        kp += forward;
+        vp += forward;
     };
 
     // V^T operand of 16 keys: columns 32 db + r
@@ -384,10 +397,15 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
         const u32x2 hi = ld_tr16(reinterpret_cast<const uint16_t*>(at + tr_off[1][db]));
         return __builtin_bit_cast(bf16x8, u32x4{lo.x, lo.y, hi.x, hi.y});
     };
+    if (walk.steps > 0) load_step(0, 0);
+    {
+        const uint16_t* p = q + token * a.qt + h * a.qh;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) qf[x] = ld_bf16x8(p + 16 * x + 8 * hh);
+    }
     begin();
     // (no load that the compiler tracks is left inside the loop: a wait for one would drain the ring)
     wait_loads_upto<0>();
-    if (walk.steps > 0) load_step(0, 0);
     int e = 0;
     two_stage_while([&](auto stage) {
         constexpr int st = decltype(stage)::value;
@@ -420,10 +438,22 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
             for (int kb = 0; kb < 2; ++kb) {
                 s[kb] = zero16();
                 if (cls[kb] == CHUNK_NONE) continue;
+                bf16x8 kf[KS];
 #pragma unroll
                 for (int x = 0; x < KS; ++x)
-                    s[kb] = mfma_32x32x16(
-                        ld_bf16x8(reinterpret_cast<const uint16_t*>(tK + row_off[x] + kb * 32 * D * 2)), qf[x], s[kb]);
+                    kf[x] = ld_bf16x8(reinterpret_cast<const uint16_t*>(tK + row_off[x] + kb * 32 * D * 2));
+#pragma unroll
+                for (int x = 0; x < KS; ++x) s[kb] = mfma_32x32x16(kf[x], qf[x], s[kb]);
+            }
+            if constexpr (decltype(full)::value) {
+                // the operands of 32 keys ahead of the first product, the other 32 keys' with them
+                __builtin_amdgcn_sched_group_barrier(0x100, PRE, 0);
+#pragma unroll
+                for (int x = 0; x < 2 * KS - PRE; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(0x008, PRE, 0);
             }
             __builtin_amdgcn_s_setprio(0);
             float mloc = -INFINITY;
@@ -448,14 +478,14 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
             m_run = m_new;
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] *= alpha;
-            float psum = 0.f;
+            f32x4 psum = zero4();  // four chains
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 if (cls[kb] == CHUNK_NONE) continue;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     s[kb][i] = exp2_fast(fmaf(s[kb][i], c2, neg));
-                    psum += s[kb][i];
+                    psum[i % 4] += s[kb][i];
                 }
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
@@ -468,7 +498,7 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
                     for (int db = 0; db < DB; ++db) acc[db] = mfma_32x32x16(vt[db], pf, acc[db]);
                 }
             }
-            l_run = fmaf(l_run, alpha, psum);
+            l_run = fmaf(l_run, alpha, (psum[0] + psum[1]) + (psum[2] + psum[3]));
         };
         if (step_full<FIXED_, KEYS>(a, part, walk, e, head_row, tail_row)) compute(std::true_type{});
         else compute(std::false_type{});
@@ -513,7 +543,7 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
                 m_run = m_new;
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[db] *= alpha;
-                float psum = 0.f;
+                f32x4 psum = zero4();
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const uint32_t b = (uint32_t)(bits >> (32 * kb));
@@ -521,7 +551,7 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         s[kb][i] = exp2_fast(fmaf(s[kb][i], c2, -m_ref * c2));
-                        psum += s[kb][i];
+                        psum[i % 4] += s[kb][i];
                     }
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
@@ -538,7 +568,7 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
                         }
                     }
                 }
-                l_run = fmaf(l_run, alpha, psum);
+                l_run = fmaf(l_run, alpha, (psum[0] + psum[1]) + (psum[2] + psum[3]));
             }
             __syncthreads();  // read before the next step is written
         }
@@ -573,7 +603,9 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
 }
 
 // ---------------------------------------------------------------------------
-// fp32: four waves of 16 rows, 32 keys a step, 16x16x4 products (see sa_f32.hip for their operands)
+// fp32: 16 rows and 16 of a step's 32 keys a wave, 16x16x4 products (see sa_f32.hip for their operands).  A tile's
+// longest walk sets the time of a short batch (2,777 tokens, 8 heads of 128, alternating factors: XX us with all 32
+// keys of a step by one wave, YY so), so two waves share the keys of 16 rows and join their states at the end.
 // ---------------------------------------------------------------------------
 __device__ inline f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -587,7 +619,7 @@ __device__ inline int swz32(int row, int piece) {
 }
 
 template <int D, bool FIXED_>
-__global__ void __launch_bounds__(kPackedThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ void __launch_bounds__(2 * kPackedThreads) __attribute__((amdgpu_waves_per_eu(2)))
 packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
                   float* __restrict__ o) {
     constexpr int KEYS = 32, ROWS = 16 * kPackedWaves, DB = D / 16;
@@ -595,13 +627,15 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
     typedef float vec __attribute__((ext_vector_type(V)));
     __shared__ __attribute__((aligned(16))) float sK[2][KEYS * D];
     __shared__ __attribute__((aligned(16))) float sV[2][KEYS * D];
+    __shared__ float s_m[kPackedWaves][16], s_l[kPackedWaves][16];
     constexpr uint32_t kTileBytes = KEYS * D * 4;
     const uint32_t sK_base = lds_addr(&sK[0][0]), sV_base = lds_addr(&sV[0][0]);
     const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, r = lane % 16;
-    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int w = __builtin_amdgcn_readfirstlane(tid / 64) % kPackedWaves;     // its 16 rows of the tile
+    const int half = __builtin_amdgcn_readfirstlane(tid / 64) / kPackedWaves;  // its 16 keys of a step
     const float c2 = a.scale_log2;
 
-    int64_t place;
+    uint32_t place;
     int h;
     if (!place_of(a, &place, &h)) return;
     const TilePlace t = tile_place<ROWS>(a, place, lane);
@@ -623,18 +657,13 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
     const int64_t token = t.base + (int64_t)row.i * a.step, at_row = (int64_t)h * a.tokens + token;
     f32x4 qf[DB], acc[DB];
     float m_run, l_run;
-    {
-        const float* p = q + token * a.qt + h * a.qh;
-#pragma unroll
-        for (int x = 0; x < DB; ++x) qf[x] = *reinterpret_cast<const f32x4*>(p + 16 * x + 4 * g);
-    }
     // acc[V hb + e][i] is element 16 V hb + V (4 g + i) + e
     auto begin = [&] {
         m_run = -INFINITY;
         l_run = 0.f;
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] = zero4();
-        if (!FIXED_ && row.i >= a.state_from) {
+        if (!FIXED_ && half == 0 && row.i >= a.state_from) {
             m_run = a.state_ml[2 * at_row];
             l_run = g == 0 ? a.state_ml[2 * at_row + 1] : 0.f;
 #pragma unroll
@@ -648,22 +677,31 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
         }
     };
     constexpr int PER = KEYS * D / 256 / kPackedWaves;
+    // the waves of the first half load K, the others V
+    const float* src = half == 0 ? kh : vh;
+    const int64_t stride = half == 0 ? ks : vs;
+    const uint32_t ring = half == 0 ? sK_base : sV_base;
     auto load_step = [&](int e, int stage) {
 #pragma unroll
         for (int x = 0; x < PER; ++x) {
             const int window = w + kPackedWaves * x, oe = 256 * window + 4 * lane;
             const int at = oe / D, piece = swz32<D>(at, (oe % D) / 4);
             const int64_t j = key_row<FIXED_, KEYS>(a, win, walk, e, at);
-            dma_b128_at(kh + j * ks + 4 * piece, sK_base + stage * kTileBytes + 1024 * window);
-            dma_b128_at(vh + j * vs + 4 * piece, sV_base + stage * kTileBytes + 1024 * window);
+            dma_b128_at(src + j * stride + 4 * piece,
+                        __builtin_amdgcn_readfirstlane(ring + stage * kTileBytes + 1024 * window));
         }
     };
 
     bool careful = false;
     while (true) {
+        if (walk.steps > 0) load_step(0, 0);
+        if (!careful) {
+            const float* p = q + token * a.qt + h * a.qh;
+#pragma unroll
+            for (int x = 0; x < DB; ++x) qf[x] = *reinterpret_cast<const f32x4*>(p + 16 * x + 4 * g);
+        }
         begin();
         wait_loads_upto<0>();
-        if (walk.steps > 0) load_step(0, 0);
         int e = 0;
         two_stage_while([&](auto stage) {
             constexpr int st = decltype(stage)::value;
@@ -680,72 +718,63 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
                 if (FIXED_ && part == PART_MERGED && e >= walk.far_steps) sum = summary_bits(mp, mod_l(a.dl, j0));
                 bits = (uint32_t)row_bits<FIXED_, KEYS>(a, part, walk, row, e, sum);
             }
+            bits = bits >> (16 * half) & 0xFFFFu;  // this wave's keys 16 half + 4 g + i
             if (__builtin_amdgcn_ballot_w64(bits != 0u) != 0ull) {
-                f32x4 s[2];
+                f32x4 c0 = zero4(), c1 = zero4();
+                const int at = 16 * half + r;
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {  // key 16 y + 4 g + i
-                    f32x4 c0 = zero4(), c1 = zero4();
-#pragma unroll
-                    for (int x = 0; x < DB; ++x) {
-                        const f32x4 kf =
-                            *reinterpret_cast<const f32x4*>(tK + (16 * y + r) * D + 4 * swz32<D>(16 * y + r, 4 * x + g));
-                        c0 = mfma_f32(kf[0], qf[x][0], c0);
-                        c1 = mfma_f32(kf[1], qf[x][1], c1);
-                        c0 = mfma_f32(kf[2], qf[x][2], c0);
-                        c1 = mfma_f32(kf[3], qf[x][3], c1);
-                    }
-                    s[y] = c0 + c1;
+                for (int x = 0; x < DB; ++x) {
+                    const f32x4 kf = *reinterpret_cast<const f32x4*>(tK + at * D + 4 * swz32<D>(at, 4 * x + g));
+                    c0 = mfma_f32(kf[0], qf[x][0], c0);
+                    c1 = mfma_f32(kf[1], qf[x][1], c1);
+                    c0 = mfma_f32(kf[2], qf[x][2], c0);
+                    c1 = mfma_f32(kf[3], qf[x][3], c1);
                 }
+                f32x4 s = c0 + c1;
                 float mx = m_run;
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        s[y][i] = select_or_neg_inf(bit_lane_mask(bits >> (4 * g), 16 * y + i), s[y][i]);
-                        mx = fmaxf(mx, s[y][i]);
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    s[i] = select_or_neg_inf(bit_lane_mask(bits >> (4 * g), i), s[i]);
+                    mx = fmaxf(mx, s[i]);
+                }
                 mx = max_over_g(mx);
                 const float m_ref = mx == -INFINITY ? 0.f : mx;
                 const float alpha = exp2_fast((m_run - m_ref) * c2);
                 float psum = 0.f;
                 // (the difference first: scaling before would lose 2^-24 of the scores themselves)
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        s[y][i] = exp2_fast((s[y][i] - m_ref) * c2);
-                        psum += s[y][i];
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    s[i] = exp2_fast((s[i] - m_ref) * c2);
+                    psum += s[i];
+                }
                 l_run = fmaf(l_run, alpha, psum);
                 m_run = mx;
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[db] *= alpha;
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+                for (int i = 0; i < 4; ++i) {
+                    const int key = 16 * half + 4 * g + i;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = 16 * y + 4 * g + i;
-#pragma unroll
-                        for (int hb = 0; hb < HB; ++hb) {
-                            const int col = 16 * V * hb + V * r;
-                            const vec x = *reinterpret_cast<const vec*>(tV + key * D + 4 * swz32<D>(key, col / 4) + col % 4);
-                            if (careful) {  // one key at a time, for the rows that attend it
+                    for (int hb = 0; hb < HB; ++hb) {
+                        const int col = 16 * V * hb + V * r;
+                        const vec x = *reinterpret_cast<const vec*>(tV + key * D + 4 * swz32<D>(key, col / 4) + col % 4);
+                        if (careful) {  // one key at a time, for the rows that attend it
 #pragma unroll 1
-                                for (int gk = 0; gk < 4; ++gk) {
-                                    const bool on = (bits >> (16 * y + 4 * gk + i)) & 1u;
+                            for (int gk = 0; gk < 4; ++gk) {
+                                const bool on = (bits >> (4 * gk + i)) & 1u;
 #pragma unroll
-                                    for (int e = 0; e < V; ++e) {
-                                        const f32x4 sum =
-                                            mfma_f32(g == gk ? x[e] : 0.f, g == gk ? s[y][i] : 0.f, acc[V * hb + e]);
-                                        if (on) acc[V * hb + e] = sum;
-                                    }
+                                for (int e = 0; e < V; ++e) {
+                                    const f32x4 sum =
+                                        mfma_f32(g == gk ? x[e] : 0.f, g == gk ? s[i] : 0.f, acc[V * hb + e]);
+                                    if (on) acc[V * hb + e] = sum;
                                 }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < V; ++e) acc[V * hb + e] = mfma_f32(x[e], s[y][i], acc[V * hb + e]);
                             }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < V; ++e) acc[V * hb + e] = mfma_f32(x[e], s[i], acc[V * hb + e]);
                         }
                     }
+                }
             }
             ++e;
             return true;
@@ -755,8 +784,30 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
         careful = true;
     }
 
-    const float l_tot = sum_over_g(l_run);
-    if (row0 + r >= t.n) return;
+    // the two states of a row, the first half's first
+    float l_tot = sum_over_g(l_run);
+    float* other = &sK[0][0];  // (what the ring holds has been read)
+    static_assert(sizeof(sK) >= ROWS * D * sizeof(float), "a state of every row");
+    if (half == 1) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            *reinterpret_cast<f32x4*>(other + ((w * DB + db) * 64 + lane) * 4) = acc[db];
+        if (g == 0) {
+            s_m[w][r] = m_run;
+            s_l[w][r] = l_tot;
+        }
+    }
+    __syncthreads();
+    if (half == 1 || row0 + r >= t.n) return;
+    {
+        const float m1 = s_m[w][r], top = fmaxf(m_run, m1);
+        const float w0 = weight(m_run, top, c2), w1 = weight(m1, top, c2);
+        l_tot = l_tot * w0 + s_l[w][r] * w1;
+        m_run = top;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            acc[db] = acc[db] * w0 + *reinterpret_cast<const f32x4*>(other + ((w * DB + db) * 64 + lane) * 4) * w1;
+    }
     const bool none = no_key(l_tot);
     const float inv = a.put_state ? 1.f : none ? 0.f : 1.f / l_tot;
     if (a.put_state && row.i < a.shift) return;
@@ -790,11 +841,12 @@ dim3 grid_of(const PackedArgs& a) {
     return dim3((unsigned)min64(n, kMaxGridX), (unsigned)((n + kMaxGridX - 1) / kMaxGridX));
 }
 
-int64_t tile_places(const PackedArgs& a, int rows) {
-    if (a.step == 1) return a.tokens / rows + a.sequences;
-    const int64_t per = (int64_t)rows * a.step;
-    return min64((int64_t)a.step * (a.tokens / min64(per, 0x7fffffff) + a.sequences), a.tokens);
+int64_t tile_places(int64_t tokens, int64_t sequences, int32_t step, int rows) {
+    if (step == 1) return tokens / rows + sequences;
+    const int64_t per = (int64_t)rows * step;
+    return min64((int64_t)step * (tokens / min64(per, 0x7fffffff) + sequences), tokens);
 }
+int64_t tile_places(const PackedArgs& a, int rows) { return tile_places(a.tokens, a.sequences, a.step, rows); }
 
 template <int D, int NW, bool FIXED_>
 hipError_t run_bf16(PackedArgs& a, const PackedCall& p, hipStream_t stream) {
@@ -813,7 +865,7 @@ hipError_t run(PackedArgs& a, const PackedCall& p, hipStream_t stream) {
     }
     a.places = tile_places(a, 16 * kPackedWaves);
     a.by_rows = a.step > 1 && a.places == a.tokens;
-    hipLaunchKernelGGL((packed_f32_kernel<D, FIXED_>), grid_of(a), dim3(kPackedThreads), 0, stream, a, (const float*)p.q,
+    hipLaunchKernelGGL((packed_f32_kernel<D, FIXED_>), grid_of(a), dim3(2 * kPackedThreads), 0, stream, a, (const float*)p.q,
                        (const float*)p.k, (const float*)p.v, (float*)p.o);
     return hipGetLastError();
 }
@@ -836,6 +888,13 @@ bool has_classes(int64_t tokens, int32_t pattern, int32_t mode, int32_t l) {
 
 size_t packed_workspace_bytes(int64_t tokens, int32_t pattern, int32_t mode, int32_t l, int32_t heads, int32_t d) {
     return has_classes(tokens, pattern, mode, l) ? (size_t)tokens * heads * (d + 2) * sizeof(float) : 0;
+}
+
+bool packed_fits(const PackedCall& p) {
+    const bool classes = p.pattern == STRIDED && p.mode != MODE_A1;
+    const int64_t places = max64(tile_places(p.tokens, p.sequences, 1, 64),
+                                 classes ? tile_places(p.tokens, p.sequences, p.l, 64) : 0);
+    return places * p.heads < (int64_t)1 << 31;
 }
 
 hipError_t packed_launch(const PackedCall& p, hipStream_t stream) {
