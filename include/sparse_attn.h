@@ -512,7 +512,7 @@ int sparse_attn_paged_decode(const int32_t* positions, int64_t max_pos, int32_t 
  * workspace: sparse_attn_packed_workspace_size bytes (0 but for strided merged heads with 2 l <
  * tokens), 16-byte aligned, contents ignored; calls that share one must not overlap.
  * SA_ERR_UNSUPPORTED for more than 2^20 sequences, 65,535 heads or 2^31 - 1,025 tokens, or where heads times
- * tokens / 64 + sequences (strided sets but A1: times tokens) reach 2^31.
+ * tokens / 32 + sequences (strided sets but A1: times tokens) reach 2^31.
  */
 int sparse_attn_packed_workspace_size(int64_t tokens, int32_t stride_l, int32_t summary_c, int32_t pattern,
                                       int32_t head_mode, int32_t heads, int32_t kv_heads, int32_t d_head,

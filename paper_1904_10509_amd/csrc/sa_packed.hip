@@ -31,7 +31,6 @@ namespace sa {
 
 namespace {
 
-constexpr int kPackedWaves = 4, kPackedThreads = 64 * kPackedWaves;
 constexpr int kNoBand = 0x7fffffff;
 
 struct PackedArgs {
@@ -47,6 +46,7 @@ struct PackedArgs {
     int32_t shift;                     // strided: nearest one
     bool by_rows;                      // classes: one place a row of the batch, live where a tile begins
     int64_t places;                    // tile places of one head
+    bool turn_heads;                   // heads of one launch have sets of different sizes
     float scale, scale_log2;
     float *state_o, *state_ml;         // states of the classes, [heads, tokens, d] and [heads, tokens, 2]
     bool put_state;                    // write them, in place of o and lse
@@ -126,6 +126,8 @@ __device__ inline bool place_of(const PackedArgs& a, uint32_t* place, int* head)
         const uint32_t each = run / 8;
         p = id / 8 / each;
         h = id % 8 * each + (id / 8 - p * each);
+        // heads that alternate between a short and a long set: every XCD takes both in turn
+        if (a.turn_heads) h = (h + p) % run;
     } else {
         p = id / run;
         h = id - p * run;
@@ -361,11 +363,11 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
 #pragma unroll
             for (int x = 0; x < PER; ++x) {
                 const int at = WR * (w + NW * x) + wrow;
-                const int32_t rows = far ? at / a.c * a.l + at % a.c : at;
+                const int32_t rows = far && even_far ? at / a.c * a.l + at % a.c : at;
                 off[x] = (uint32_t)((rows * ks + 8 * chunk) * 2);
             }
             const int64_t j = far ? win : walk.lo;
-            forward = (far ? (int64_t)(KEYS / a.c) * a.l : KEYS) * ks;
+            forward = (far ? (int64_t)(KEYS / a.c) * a.l : KEYS) * ks;  // (0 and unused where c > KEYS)
             kp = kh + j * ks;
             vp = vh + j * vs;
         }
@@ -618,21 +620,23 @@ __device__ inline int swz32(int row, int piece) {
     return piece ^ (row & (D / 4 < 16 ? D / 4 - 1 : 15));
 }
 
+constexpr int kGroups = 2;  // groups of 16 rows of a tile: their waves and the keys' halves fill the four SIMDs
+
 template <int D, bool FIXED_>
-__global__ void __launch_bounds__(2 * kPackedThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ void __launch_bounds__(128 * kGroups) __attribute__((amdgpu_waves_per_eu(2)))
 packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
                   float* __restrict__ o) {
-    constexpr int KEYS = 32, ROWS = 16 * kPackedWaves, DB = D / 16;
+    constexpr int KEYS = 32, ROWS = 16 * kGroups, DB = D / 16;
     constexpr int V = D >= 64 ? 4 : 2, HB = D / (16 * V);  // neighbours in d per read of V, reads per row
     typedef float vec __attribute__((ext_vector_type(V)));
     __shared__ __attribute__((aligned(16))) float sK[2][KEYS * D];
     __shared__ __attribute__((aligned(16))) float sV[2][KEYS * D];
-    __shared__ float s_m[kPackedWaves][16], s_l[kPackedWaves][16];
+    __shared__ float s_m[kGroups][16], s_l[kGroups][16];
     constexpr uint32_t kTileBytes = KEYS * D * 4;
     const uint32_t sK_base = lds_addr(&sK[0][0]), sV_base = lds_addr(&sV[0][0]);
     const int tid = threadIdx.x, lane = tid % 64, g = lane / 16, r = lane % 16;
-    const int w = __builtin_amdgcn_readfirstlane(tid / 64) % kPackedWaves;     // its 16 rows of the tile
-    const int half = __builtin_amdgcn_readfirstlane(tid / 64) / kPackedWaves;  // its 16 keys of a step
+    const int w = __builtin_amdgcn_readfirstlane(tid / 64) % kGroups;     // its 16 rows of the tile
+    const int half = __builtin_amdgcn_readfirstlane(tid / 64) / kGroups;  // its 16 keys of a step
     const float c2 = a.scale_log2;
 
     uint32_t place;
@@ -676,7 +680,7 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
                 }
         }
     };
-    constexpr int PER = KEYS * D / 256 / kPackedWaves;
+    constexpr int PER = KEYS * D / 256 / kGroups;
     // the waves of the first half load K, the others V
     const float* src = half == 0 ? kh : vh;
     const int64_t stride = half == 0 ? ks : vs;
@@ -684,7 +688,7 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
     auto load_step = [&](int e, int stage) {
 #pragma unroll
         for (int x = 0; x < PER; ++x) {
-            const int window = w + kPackedWaves * x, oe = 256 * window + 4 * lane;
+            const int window = w + kGroups * x, oe = 256 * window + 4 * lane;
             const int at = oe / D, piece = swz32<D>(at, (oe % D) / 4);
             const int64_t j = key_row<FIXED_, KEYS>(a, win, walk, e, at);
             dma_b128_at(src + j * stride + 4 * piece,
@@ -863,9 +867,9 @@ hipError_t run(PackedArgs& a, const PackedCall& p, hipStream_t stream) {
         if (D == 128 || tile_places(a, 128) * a.run_heads >= kWidePlaces) return run_bf16<D, 4, FIXED_>(a, p, stream);
         if constexpr (D < 128) return run_bf16<D, 2, FIXED_>(a, p, stream);
     }
-    a.places = tile_places(a, 16 * kPackedWaves);
+    a.places = tile_places(a, 16 * kGroups);
     a.by_rows = a.step > 1 && a.places == a.tokens;
-    hipLaunchKernelGGL((packed_f32_kernel<D, FIXED_>), grid_of(a), dim3(2 * kPackedThreads), 0, stream, a, (const float*)p.q,
+    hipLaunchKernelGGL((packed_f32_kernel<D, FIXED_>), grid_of(a), dim3(128 * kGroups), 0, stream, a, (const float*)p.q,
                        (const float*)p.k, (const float*)p.v, (float*)p.o);
     return hipGetLastError();
 }
@@ -892,8 +896,8 @@ size_t packed_workspace_bytes(int64_t tokens, int32_t pattern, int32_t mode, int
 
 bool packed_fits(const PackedCall& p) {
     const bool classes = p.pattern == STRIDED && p.mode != MODE_A1;
-    const int64_t places = max64(tile_places(p.tokens, p.sequences, 1, 64),
-                                 classes ? tile_places(p.tokens, p.sequences, p.l, 64) : 0);
+    const int64_t places = max64(tile_places(p.tokens, p.sequences, 1, 32),
+                                 classes ? tile_places(p.tokens, p.sequences, p.l, 32) : 0);
     return places * p.heads < (int64_t)1 << 31;
 }
 
@@ -918,6 +922,7 @@ hipError_t packed_launch(const PackedCall& p, hipStream_t stream) {
     a.scale = p.scale;
     a.scale_log2 = p.scale * kLog2eHost;
     a.lse = p.lse;
+    a.turn_heads = p.pattern == FIXED && p.mode == MODE_INTERLEAVED;
     if (p.pattern == FIXED) return run_d<true>(a, p, stream);
 
     PackedArgs band = a, cls = a;
