@@ -18,8 +18,9 @@
 // and takes at most tokens / Q + sequences in all.  Places behind a sequence's last tile are
 // empty.
 //
-// What bounds it: long walks the matrix products and the exponentials beside them, short ones
-// (a prompt of hundreds of tokens) the steps' latency.
+// What bounds it: long walks the matrix products and the exponentials beside them, which share a SIMD's time (32
+// heads of 128, 4 x 4,096 dense: 680 us, 809 TFLOP/s; products 36%, vector instructions 43% of it), short ones the
+// steps' latency and, strided merged, the states' way through memory.
 #include "sa_finite.h"
 #include "sa_internal.h"
 #include "sa_mask.h"
@@ -350,7 +351,8 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
     };
     // One step's K and V rows to a ring stage.  Steps whose rows lie at the same distances from their first one (keys
     // one behind the other; columns in runs of c that divide 64) take their addresses from a scalar that moves on by a
-    // constant; in the others, and where rows would lie behind the sequence, every lane forms its row's.
+    // constant; in the others, and where rows would lie behind the sequence, every lane forms its row's.  (32 heads of
+    // 128, 4 x 4,096 dense: 685 us; the scalar formed anew for every step 728, per 1 KiB window 740.)
     const bool even = ks == vs && 64 * ks < (int64_t)1 << 30;
     const bool even_far = FIXED_ && even && KEYS % a.c == 0 && (KEYS / a.c) * (int64_t)a.l * ks < (int64_t)1 << 30;
     uint32_t off[PER];
@@ -480,7 +482,7 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
             m_run = m_new;
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] *= alpha;
-            f32x4 psum = zero4();  // four chains
+            f32x4 psum = zero4();  // four chains (d = 64, 2 x 8,192 dense, 16 heads: 399 -> 392 us)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 if (cls[kb] == CHUNK_NONE) continue;
@@ -605,9 +607,10 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
 }
 
 // ---------------------------------------------------------------------------
-// fp32: 16 rows and 16 of a step's 32 keys a wave, 16x16x4 products (see sa_f32.hip for their operands).  A tile's
-// longest walk sets the time of a short batch (2,777 tokens, 8 heads of 128, alternating factors: XX us with all 32
-// keys of a step by one wave, YY so), so two waves share the keys of 16 rows and join their states at the end.
+// fp32: 16 rows and 16 of a step's 32 keys a wave, 16x16x4 products (see sa_f32.hip for their operands).  Two waves
+// share the keys of 16 rows and join their states at the end, so that a tile's walk is spread over the four SIMDs: a
+// ragged batch waits for its longest (2,777 tokens at most, 8 heads of 128, alternating factors: 113 us with four
+// groups of 16 rows and a wave for each, 104 so; dense 4 x 2,048, 8 heads: 423 us, 81 TFLOP/s, the products 57% of it).
 // ---------------------------------------------------------------------------
 __device__ inline f32x4 mfma_f32(float a, float b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
@@ -838,7 +841,9 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
 // Launches
 // ---------------------------------------------------------------------------
 constexpr int64_t kMaxGridX = 1 << 20;     // workgroups along x; along y the rest
-constexpr int64_t kWidePlaces = 1024;      // tiles of 128 rows from so many workgroups on
+// Tiles of 128 rows from so many workgroups on, which fill the chip; below, tiles of 64 (d = 128: always 128, as
+// two waves a workgroup would leave its 64 KB of LDS half used).
+constexpr int64_t kWidePlaces = 1024;
 
 dim3 grid_of(const PackedArgs& a) {
     const int64_t n = a.places * a.run_heads;

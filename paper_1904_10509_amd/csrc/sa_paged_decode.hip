@@ -39,6 +39,7 @@ struct PagedArgs {
     int32_t sub, max_pos, l, sc;
     int32_t least;               // keys of a range, at least
     int32_t batch;
+    int32_t each;                // ranges of every sequence at most; 0: `splits` of the whole batch (share_of)
     int2* cuts;                  // [batch, heads]: first range and ranges of a row
     DivL dc;
     int64_t qsb, qsh, osb, osh;  // strides of q and o
@@ -55,9 +56,10 @@ struct PagedArgs {
 
 // How the sets of a batch are cut for one head: every sequence into equal ranges of at most `per` keys, all of
 // them about `target` (PagedArgs::splits) ranges together, numbered through the batch.  Sequences of different
-// lengths then take as long as each other: a fixed number of ranges for each, 16 sequences between 866 and 32,767
-// keys (4 cache heads of 128, 8 query heads each) took 93.2 us, this way XX.  Every wave makes the sums by itself, a
-// sequence a lane.
+// lengths then take as long as each other: with a fixed number of ranges for each, 16 sequences between 866 and
+// 32,767 keys (4 cache heads of 128, 8 query heads each) took 93.2 us, this way 53.8; of one length, 94.9 | 99.9, for
+// the sums.  Every wave makes them by itself, a sequence a lane (64
+// sequences at most).
 struct Share {
     int64_t b;        // the sequence of a range (-1: there is none)
     int32_t base;     // ranges of the sequences before it
@@ -79,43 +81,28 @@ __device__ inline int32_t sum_upto(int32_t x) {
     return x;
 }
 __device__ inline Share share_of(const PagedArgs& a, int h, int32_t range, int lane) {
-    // in pieces of 64 keys, rounded up: 64 sequences' are within 31 bits
-    const uint32_t mine = keys_of(a, h, lane);  // the first 64 sequences: read once
-    uint64_t total = 0;
-    for (int64_t b0 = 0; b0 < a.batch; b0 += 64) {
-        const uint32_t count = b0 == 0 ? mine : keys_of(a, h, b0 + lane);
-        total += (uint32_t)__builtin_amdgcn_readlane(sum_upto((int32_t)((count >> 6) + (count % 64 != 0))), 63);
+    const uint32_t count = keys_of(a, h, lane);
+    // in pieces of 64 keys, rounded up: all sequences' are within 32 bits
+    const uint32_t total =
+        (uint32_t)__builtin_amdgcn_readlane(sum_upto((int32_t)((count >> 6) + (count % 64 != 0))), 63);
+    uint32_t per = max(min(total / a.splits + (total % a.splits != 0), 1u << 25) << 6, (uint32_t)a.least);
+    int32_t n, upto;
+    for (int i = 0;; ++i) {
+        n = count == 0 ? 0 : (int32_t)((count - 1) / per + 1);
+        upto = sum_upto(n);  // ranges up to this sequence
+        const int32_t all = __builtin_amdgcn_readlane(upto, 63);
+        if (all <= a.splits || i == 3) break;
+        // rounded up for each sequence, they are more than `splits`: longer ones
+        per = (uint32_t)min64(((int64_t)per * all / a.splits + 64) & ~63ll, (int64_t)1 << 31);
     }
-    const uint32_t pieces = total >> 31 == 0 ? ((uint32_t)total + a.splits - 1) / a.splits
-                                             : (uint32_t)min((total + a.splits - 1) / a.splits, (uint64_t)1 << 25);
-    uint32_t per = max(pieces << 6, (uint32_t)a.least);
-    if (a.batch <= 64) {
-        // rounded up for each sequence, they can be more than `splits`: longer ones, until they are not
-        for (int i = 0; i < 3; ++i) {
-            const int32_t n = __builtin_amdgcn_readlane(sum_upto(mine == 0 ? 0 : (int32_t)((mine - 1) / per + 1)), 63);
-            if (n <= a.splits) break;
-            per = (uint32_t)min64(((int64_t)per * n / a.splits + 64) & ~63ll, (int64_t)1 << 31);
-        }
-    }
-    Share s{-1, 0, 0, 0};
-    for (int64_t b0 = 0; b0 < a.batch; b0 += 64) {
-        const uint32_t count = b0 == 0 ? mine : keys_of(a, h, b0 + lane);
-        const int32_t n = count == 0 ? 0 : (int32_t)((count - 1) / per + 1);
-        const int32_t end = s.base + sum_upto(n);  // ranges up to this sequence
-        const uint64_t up = __builtin_amdgcn_ballot_w64(end > range);
-        if (up) {
-            const int at = __builtin_ctzll(up);
-            s.b = b0 + at;
-            s.ranges = __builtin_amdgcn_readlane(n, at);
-            s.base = __builtin_amdgcn_readlane(end, at) - s.ranges;
-            s.count = (uint32_t)__builtin_amdgcn_readlane((int)count, at);
-            return s;
-        }
-        s.base = __builtin_amdgcn_readlane(end, 63);
-    }
-    return s;
+    const uint64_t up = __builtin_amdgcn_ballot_w64(upto > range);
+    if (!up) return {-1, 0, 0, 0};
+    const int at = __builtin_ctzll(up);
+    const int32_t ranges = __builtin_amdgcn_readlane(n, at);
+    return {at, __builtin_amdgcn_readlane(upto, at) - ranges, ranges, (uint32_t)__builtin_amdgcn_readlane((int)count, at)};
 }
-// The row's first range leaves both numbers for the join; a row without a key has none.
+// The row's first range leaves both numbers for the join (which forming the sums again took 1.8 us longer); a row
+// without a key has none.
 __device__ inline int PagedArgs::ranges(int64_t b, int64_t h, int64_t* first, int64_t* step) const {
     *step = heads;
     *first = 0;
@@ -197,16 +184,14 @@ __device__ inline void scores(const uint8_t* rows, const Query<D, uint16_t>& q, 
 template <int D>
 __device__ inline void scores(const uint8_t* rows, const Query<D, float>& q, int g, int r, f32x4* s) {
     const float* row = reinterpret_cast<const float*>(rows + r * Step<D, float>::PITCH);
-    f32x4 a = zero4(), b = zero4();  // two chains: no product waits for the one before it
+    f32x4 part[4] = {zero4(), zero4(), zero4(), zero4()};  // four short sums: half the rounding of one long one
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
         const f32x4 k = *reinterpret_cast<const f32x4*>(row + 16 * x + 4 * g);
-        a = mfma_f32(k[0], q.x[x][0], a);
-        b = mfma_f32(k[1], q.x[x][1], b);
-        a = mfma_f32(k[2], q.x[x][2], a);
-        b = mfma_f32(k[3], q.x[x][3], b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[i] = mfma_f32(k[i], q.x[x][i], part[i]);
     }
-    s[0] = a + b;
+    s[0] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 // acc += V^T P.  bf16: acc[t][i] is element 16 t + 4 g + i of head column r; fp32: acc[V hb + e][i]
@@ -277,8 +262,19 @@ paged_split_kernel(PagedArgs a, const T* __restrict__ q, float* __restrict__ par
     if constexpr (DIRECT) {
         t1 = keys_of(a, h0, b);
     } else {
-        const Share s = share_of(a, h0, range, lane);
-        if (s.b < 0) return;
+        Share s;
+        if (a.each > 0) {
+            s.b = range / a.each;
+            s.base = (int32_t)s.b * a.each;
+            s.count = keys_of(a, h0, s.b);
+            if (s.count == 0) return;
+            const uint32_t per = max((s.count + a.each - 1) / a.each, (uint32_t)a.least);
+            s.ranges = (int32_t)((s.count - 1) / per + 1);
+            if (range - s.base >= s.ranges) return;
+        } else {
+            s = share_of(a, h0, range, lane);
+            if (s.b < 0) return;
+        }
         b = s.b;
         // equal ranges of the sequence
         const uint32_t per = (s.count + s.ranges - 1) / s.ranges;
@@ -456,6 +452,33 @@ paged_split_kernel(PagedArgs a, const T* __restrict__ q, float* __restrict__ par
     }
 }
 
+// How a call's sets are cut.
+struct Cut {
+    int32_t splits;  // ranges of the batch, one more for each sequence at most; 0: every sequence is one range
+    int32_t each;    // > 0: so many of every sequence instead
+    int64_t ranges(int64_t batch) const { return each > 0 ? batch * each : splits + batch; }
+};
+//   One range a sequence up to 256 keys: there is nothing to join.
+//   Up to 64 sequences: as many ranges as fill the workgroups that run at once (2 a compute unit for d = 128, whose
+//   rows take 68 KB of LDS, 3 for d = 64, 5 for d = 32), so that they end together (one sequence of 32,768, 4 cache
+//   heads of 128: 21.3 us, twice as many 29.2; 16 sequences of 866 to 32,767: 53.8 | 63.4), or four for each sequence.
+//   More sequences, whose sums every workgroup would form at length: a number for each, four or what leaves a range
+//   2,048 keys within 32,768 workgroups; short ranges even out over several rounds.
+// No range has fewer than 128 keys, one chunk a wave (two of fp32).
+constexpr int32_t kLeastKeys = 128;
+Cut cut_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t batch, int64_t units, int d) {
+    const int64_t count = largest_set(pattern, mode, sub, max_pos, l, c);
+    if (count <= 256) return {0, 0};
+    const int64_t finest = (count + kLeastKeys - 1) / kLeastKeys;
+    if (batch > 64) {
+        const int64_t each = max64(4, min64((count + 2047) / 2048, 32768 / (batch * units)));
+        return {1, (int32_t)min64(each, finest)};
+    }
+    const int64_t places = 256 * (d == 128 ? 2 : d == 64 ? 3 : 5) / units;  // of one unit
+    const int64_t n = places >= 2 * batch ? places : 4 * batch;
+    return {(int32_t)max64(1, min64(n, batch * finest)), 0};
+}
+
 template <int D, typename T>
 hipError_t launch(const PagedArgs& a, const void* q, void* o, float* lse, float* part, hipStream_t stream) {
     const dim3 wg(kWaves * 64);
@@ -464,32 +487,19 @@ hipError_t launch(const PagedArgs& a, const void* q, void* o, float* lse, float*
                            (const T*)q, part, (T*)o, lse);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((paged_split_kernel<D, T, false>), dim3((unsigned)((int64_t)(a.splits + a.batch) * a.u.units)), wg, 0,
-                       stream, a, (const T*)q, part, (T*)o, lse);
-    return step_combine<D, T>(a, a.batch, 2 * a.splits / a.batch, part, o, lse, stream);
-}
-
-// Ranges that a call's sets are cut into (about; one more for each sequence at most), 0 where every sequence is one.
-//   One up to 256 keys: there is nothing to join.
-//   Else as many as fill the workgroups that run at once (2 a compute unit for d = 128, whose rows take 68 KB of
-//   LDS, 3 for d = 64, 5 for d = 32), so that they end together;
-//   with more sequences than that allows, four for each: short ranges even out over several rounds.
-// No range has fewer than 128 keys, one chunk a wave (two of fp32).
-constexpr int32_t kLeastKeys = 128;
-int splits_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t batch, int64_t units, int d) {
-    const int64_t count = largest_set(pattern, mode, sub, max_pos, l, c);
-    if (count <= 256) return 0;
-    const int64_t places = 256 * (d == 128 ? 2 : d == 64 ? 3 : 5) / units;  // of one unit
-    const int64_t n = places >= 2 * batch ? places : 4 * batch;
-    return (int)max64(1, min64(n, batch * ((count + kLeastKeys - 1) / kLeastKeys)));
+    const int64_t ranges = Cut{a.splits, a.each}.ranges(a.batch);
+    hipLaunchKernelGGL((paged_split_kernel<D, T, false>), dim3((unsigned)(ranges * a.u.units)), wg, 0, stream, a,
+                       (const T*)q, part, (T*)o, lse);
+    return step_combine<D, T>(a, a.batch, a.each > 0 ? a.each : 2 * a.splits / a.batch, part, o, lse, stream);
 }
 
 }  // namespace
 
 size_t paged_decode_workspace_bytes(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c,
                                     int batch, int heads, int kv_heads, int d) {
-    const int splits = splits_of(pattern, mode, sub, max_pos, l, c, batch, head_units(mode, sub, heads, kv_heads).units, d);
-    return splits == 0 ? 0 : (size_t)(splits + batch) * heads * (d + 2) * sizeof(float) + (size_t)batch * heads * sizeof(int2);
+    const Cut cut = cut_of(pattern, mode, sub, max_pos, l, c, batch, head_units(mode, sub, heads, kv_heads).units, d);
+    if (cut.splits == 0) return 0;
+    return (size_t)cut.ranges(batch) * heads * (d + 2) * sizeof(float) + (size_t)batch * heads * sizeof(int2);
 }
 
 hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l,
@@ -509,7 +519,9 @@ hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_
     a.kv_heads = kv_heads;
     a.u = head_units(mode, sub, heads, kv_heads);
     a.batch = batch;
-    a.splits = splits_of(pattern, mode, sub, max_pos, l, c, batch, a.u.units, d);
+    const Cut cut = cut_of(pattern, mode, sub, max_pos, l, c, batch, a.u.units, d);
+    a.splits = cut.splits;
+    a.each = cut.each;
     a.least = kLeastKeys;
     a.sub = sub;
     a.max_pos = max_pos;
@@ -522,7 +534,7 @@ hipError_t paged_decode_launch(const PagedStep& p, int pattern, int mode, int32_
     a.osh = o_strides[1];
     a.scale_log2 = scale * kLog2eHost;
     float* part = static_cast<float*>(workspace);
-    a.cuts = reinterpret_cast<int2*>(part + (int64_t)(a.splits + batch) * heads * (d + 2));  // (d + 2 is even)
+    a.cuts = reinterpret_cast<int2*>(part + cut.ranges(batch) * heads * (d + 2));  // (d + 2 is even)
     if (dtype == 1) {
         switch (d) {
         case 32: return launch<32, uint16_t>(a, q, o, lse, part, stream);

@@ -194,3 +194,20 @@ def test_large_scores():
         o, lse = sa.paged_decode(q, cache, table, positions, 1000, 0, S, A1, softmax_scale=1.0)
         torch.cuda.synchronize()
         check(o, lse, q, values, [399, 100], 1000, 0, S, A1, scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("batch", [63, 64, 65, 200])
+def test_many_sequences(batch, dtype):
+    """Sets of very different sizes, some empty, cut by their sum and (from 65 sequences on) each by itself."""
+    rng = np.random.RandomState(batch)
+    at = np.exp(rng.uniform(0, np.log(1500), batch)).astype(int) * (rng.rand(batch) < 0.9) - 1
+    at[batch // 2] = 1499
+    at = at.tolist()
+    cache, table, values = make(at, 1, 1500, 32, dtype, 16, 3)
+    q = torch.randn((batch, 3, 32), generator=torch.Generator().manual_seed(6)).to(dtype).to(device())
+    positions = torch.tensor(at, dtype=torch.int32, device=device())
+    for pattern, mode, l, c in ((S, A1, 2000, 0), (F, IL, 100, 60)):
+        o, lse = sa.paged_decode(q, cache, table, positions, l, c, pattern, mode)
+        torch.cuda.synchronize()
+        check(o, lse, q, values, at, l, c, pattern, mode)
