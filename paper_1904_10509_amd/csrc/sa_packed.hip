@@ -38,7 +38,7 @@ struct PackedArgs {
     const int32_t* starts;
     int32_t sequences, tokens;
     int64_t qt, qh, kt, kh, vt, vh, ot, oh;
-    int32_t heads, group;              // query heads; of one key head
+    int32_t group;                     // query heads of a key head
     int32_t head0, head_step, run_heads;  // heads of this launch: head0, head0 + head_step, ...
     int32_t mode, sub, l, c;
     DivL dl, dc;
@@ -48,7 +48,7 @@ struct PackedArgs {
     bool by_rows;                      // classes: one place a row of the batch, live where a tile begins
     int64_t places;                    // tile places of one head
     bool turn_heads;                   // heads of one launch have sets of different sizes
-    float scale, scale_log2;
+    float scale_log2;
     float *state_o, *state_ml;         // states of the classes, [heads, tokens, d] and [heads, tokens, 2]
     bool put_state;                    // write them, in place of o and lse
     int32_t state_from;                // rows from here on have one to go on from (0x7fffffff: none)
@@ -912,7 +912,6 @@ hipError_t packed_launch(const PackedCall& p, hipStream_t stream) {
     a.sequences = p.sequences;
     a.tokens = (int32_t)p.tokens;
     a.qt = p.qt, a.qh = p.qh, a.kt = p.kt, a.kh = p.kh, a.vt = p.vt, a.vh = p.vh, a.ot = p.ot, a.oh = p.oh;
-    a.heads = p.heads;
     a.group = p.heads / p.kv_heads;
     a.head_step = 1;
     a.run_heads = p.heads;
@@ -924,7 +923,6 @@ hipError_t packed_launch(const PackedCall& p, hipStream_t stream) {
     a.dc = make_divl(p.c > 0 ? p.c : 1);
     a.step = 1;
     a.state_from = kNoBand;
-    a.scale = p.scale;
     a.scale_log2 = p.scale * kLog2eHost;
     a.lse = p.lse;
     a.turn_heads = p.pattern == FIXED && p.mode == MODE_INTERLEAVED;
