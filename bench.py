@@ -252,7 +252,8 @@ def decode_bench(args):
     """Time per decoding step (sparse_attn_decode at positions n - steps .. n - 1,
     one per step, as in generation) and the bandwidth of the K / V rows it
     reads (|S_pos| rows of K and of V per (sequence, head)) against HBM; the same
-    over an 8-bit cache of these keys and values (sparse_attn_decode8)."""
+    over an 8-bit cache of these keys and values (sparse_attn_decode8) and over a
+    cache in pages of 64 tokens in no order (sparse_attn_paged_decode)."""
     import torch
 
     from paper_1904_10509_amd import sparse_attn as sa
@@ -306,6 +307,25 @@ def decode_bench(args):
                        workspace=ws8)
 
         us8 = timed(step8)
+        del cache
+        # and in pages
+        held, fresh = (torch.full((c["batch"],), x, dtype=torch.int32, device=dev) for x in (0, c["n"]))
+        per = -(-c["n"] // 64)
+        table = torch.empty((c["batch"], per), dtype=torch.int32, device=dev)
+        free = torch.randperm(c["batch"] * per, generator=g, device=dev).to(torch.int32)
+        slots = sa.page_tables(table, held, fresh, free, 64, c["batch"] * c["n"]).slots
+        paged = sa.build_paged_cache(c["batch"] * per, c["heads"], 64, c["d"], device=dev)
+        for b in range(c["batch"]):
+            sa.paged_store(paged, kc[b].transpose(0, 1), vc[b].transpose(0, 1), slots[b * c["n"]:(b + 1) * c["n"]])
+        wsp = torch.empty(max(16, sa.sparse_attn_paged_decode_workspace_size(
+            c["n"] - 1, c["l"], c["c"], c["pattern"], sa.SA_MODE_MERGED, c["batch"], c["heads"], c["heads"], c["d"],
+            sa.SA_BF16)), dtype=torch.uint8, device=dev)
+
+        def step_paged(s):
+            sa.paged_decode(qs[s], paged, table, places[s], c["l"], c["c"], c["pattern"], sa.SA_MODE_MERGED, out=o, lse=lse,
+                            workspace=wsp)
+
+        us_paged = timed(step_paged)
         # |S_pos| of the merged sets (closed forms of Sec. 4.3, the same for every
         # summary subblock), averaged over the timed positions
         rows = 0
@@ -327,7 +347,12 @@ def decode_bench(args):
                                          "tokens_per_s": c["batch"] / (us8 * 1e-6),
                                          "roofline": {"bound": "hbm", "achieved": gbs8, "peak": HBM_PEAK_GBS,
                                                       "unit": "GB/s", "frac": gbs8 / HBM_PEAK_GBS}}
-        del kc, vc, cache
+        gbs_paged = kv_bytes / (us_paged * 1e-6) / 1e9
+        out["shapes"][name]["paged"] = {"us_per_step": us_paged, "kv_bytes_per_step": kv_bytes,
+                                        "tokens_per_s": c["batch"] / (us_paged * 1e-6),
+                                        "roofline": {"bound": "hbm", "achieved": gbs_paged, "peak": HBM_PEAK_GBS,
+                                                     "unit": "GB/s", "frac": gbs_paged / HBM_PEAK_GBS}}
+        del kc, vc, paged, slots
         torch.cuda.empty_cache()
     print(json.dumps(out), flush=True)
 
