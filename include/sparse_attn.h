@@ -449,7 +449,8 @@ int sparse_attn_decode8(const int32_t* positions, int64_t max_pos, int32_t strid
  * Negative lengths are taken as 0, a held length above max_pages * page as that.  Rows that have no
  * place have position and slot -1 (padding, and tokens behind the table's last page) or slot -1 (the
  * list was short: taken > free_count, and the table's entry is -1).  Rows beyond `tokens` do not
- * count: starts ends there, and no pages are taken for them.  The outputs must not overlap.
+ * count: starts ends there, and no pages are taken for them.  Outputs and the table that overlap each other, or an
+ * output or the table that overlaps an input, are SA_ERR_INVALID.
  * SA_ERR_UNSUPPORTED for more than 8,000 sequences or a table of 2^31 tokens or more a sequence.
  */
 int sparse_attn_page_tables(int32_t sequences, const int32_t* held, const int32_t* fresh, int32_t page,

@@ -367,6 +367,20 @@ int check_packed(int64_t tokens, int32_t l, int32_t c, int32_t pattern, int32_t 
     return SA_OK;
 }
 
+// Whether n integers at p lie apart from m others at q.
+bool ints_apart(const int32_t* p, int64_t n, const int32_t* q, int64_t m) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return n == 0 || m == 0 || a + 4 * (uint64_t)n <= b || b + 4 * (uint64_t)m <= a;
+}
+
+// The same of a table's rows, `width` integers each and `stride` from one to the next.
+bool ints_apart_of_rows(const int32_t* p, int64_t n, const int32_t* table, int64_t rows, int64_t width, int64_t stride) {
+    if (n == 0) return true;
+    const int64_t begin = ((intptr_t)p - (intptr_t)table) / 4, end = begin + n;  // from the table's first entry on
+    const int64_t row = begin < width ? 0 : (begin - width) / stride + 1;  // the first one that ends behind `begin`
+    return row >= rows || row * stride >= end;
+}
+
 // A cache in pages and the shape of what it holds.
 int check_pages(const void* k, const void* v, const int64_t* strides, int64_t pages, int32_t page, int32_t kv_heads,
                 int32_t d, int32_t dtype, sa::PagedCache* out, int32_t* shift) {
@@ -860,6 +874,21 @@ int sparse_attn_page_tables(int32_t sequences, const int32_t* held, const int32_
                           (const void*)taken})
         if (!aligned4(p)) return SA_ERR_INVALID;
     if (sequences > sa::kMaxTableSequences || (int64_t)max_pages * page > INT32_MAX) return SA_ERR_UNSUPPORTED;
+    // Workgroups read the lengths and the list while others write: an output that lay in an input (`last` in `held`,
+    // say) would move the places of entries after they were counted.
+    const struct { const int32_t* p; int64_t n; } outs[] = {{starts, sequences + 1}, {positions, tokens}, {slots, tokens},
+                                                            {last, sequences}, {taken, 1}},
+                                                  ins[] = {{held, sequences}, {fresh, sequences}, {free_pages, free_count}};
+    const int64_t row_stride = sequences > 1 ? table_stride : max_pages;
+    for (const auto& x : outs) {
+        for (const auto& y : outs)
+            if (&x < &y && !ints_apart(x.p, x.n, y.p, y.n)) return SA_ERR_INVALID;
+        for (const auto& y : ins)
+            if (!ints_apart(x.p, x.n, y.p, y.n)) return SA_ERR_INVALID;
+        if (!ints_apart_of_rows(x.p, x.n, table, sequences, max_pages, row_stride)) return SA_ERR_INVALID;
+    }
+    for (const auto& y : ins)
+        if (!ints_apart_of_rows(y.p, y.n, table, sequences, max_pages, row_stride)) return SA_ERR_INVALID;
     sa::PageTables a;
     a.sequences = sequences;
     a.held = held;

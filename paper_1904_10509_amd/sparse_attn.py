@@ -858,7 +858,7 @@ def page_tables(table, held, fresh, free, page, tokens, out=None, stream=None):
     """The bookkeeping of a batch of sequences that hold ``held`` tokens in the cache and bring ``fresh`` ones (int32
     [sequences] on the device), packed into ``tokens`` rows: fills the new pages' entries of ``table`` (int32
     [sequences, max_pages], in place) from the front of the list ``free`` (int32), and returns a ``PageMap``.  ``out``: a
-    ``PageMap`` to write into."""
+    ``PageMap`` to write into, apart from the inputs."""
     device = table.device
     if device.type != "cuda":
         raise ValueError("table must be on the GPU")

@@ -161,3 +161,30 @@ def test_store_beyond_32_bits():
     torch.cuda.synchronize()
     for t, s in enumerate(slots.tolist()):
         assert torch.equal(cache.k[s // page, :, s % page], x[t]) and torch.equal(cache.v[s // page, :, s % page], -x[t])
+
+
+def test_lengths_between_the_rows_of_a_table():
+    """Lengths and outputs that lie between a table's rows are no part of it; a call whose `last` is its `held` is
+    refused, and nothing is written."""
+    dev = device()
+    buf = torch.full((4, 32), -9, dtype=torch.int32, device=dev)
+    table, held, fresh = buf[:3, :4], buf[0, 4:7], buf[0, 7:10]
+    free = buf[1, 4:12]
+    out = sa.PageMap(buf[2, 4:8], buf[1, 12:32], buf[3, :20], buf[2, 8:11], buf[2, 11:12])
+    held.copy_(ints([5, 16, 0], dev))
+    fresh.copy_(ints([12, 3, 2], dev))
+    free.copy_(torch.arange(50, 58))
+    table.copy_(ints([[40, -9, -9, -9], [41, -9, -9, -9], [-9] * 4], dev))
+    want, lengths = table.cpu().numpy().astype(np.int64), [5, 16, 0]
+    torch.cuda.synchronize()
+    before = buf.clone()
+    with pytest.raises(sa.SparseAttnError):
+        sa.page_tables(table, held, fresh, free, 16, 20, out=sa.PageMap(out.starts, out.positions, out.slots, held, out.taken))
+    torch.cuda.synchronize()
+    assert torch.equal(buf, before)
+    sa.page_tables(table, held, fresh, free, 16, 20, out=out)
+    torch.cuda.synchronize()
+    expect = ref.page_tables(want, lengths, [12, 3, 2], list(range(50, 58)), 16, 20)
+    assert np.array_equal(table.cpu().numpy(), want) and held.tolist() == lengths
+    for name, w in zip(("starts", "positions", "slots", "last", "taken"), expect):
+        assert np.array_equal(getattr(out, name).cpu().numpy(), w), name

@@ -122,3 +122,26 @@ def test_packed_workspace(L):
     assert need(pattern=sa.SA_FIXED, c=32) == 0
     with pytest.raises(sa.SparseAttnError):
         need(kv=3)
+
+
+# arguments of a call on 4 sequences of 10 entries 16 apart, 50 rows and a list of 100, each at an address of its own
+SPACED = dict(TABLES, held=0x100000, fresh=0x110000, table=0x120000, table_stride=16, free=0x130000, starts=0x140000,
+              positions=0x150000, slots=0x160000, last=0x170000, taken=0x180000)
+
+
+@pytest.mark.parametrize("name,at", [
+    ("last", "held"), ("last", "fresh"), ("starts", "held"), ("positions", "fresh"), ("taken", "free"), ("slots", "free"),
+    ("positions", "slots"), ("last", "starts"), ("taken", "last"), ("starts", "table"), ("table", "held"), ("table", "free"),
+    ("fresh", "table"), ("taken", "positions"),
+])
+@pytest.mark.parametrize("by", [0, 4, -4])
+def test_page_tables_that_overlap(L, name, at, by):
+    """An output in an input or in another output, whole or by an element at either end, would be read by one workgroup
+    while another writes it."""
+    size = dict(held=4, fresh=4, table=3 * 16 + 10, free=100, starts=5, positions=50, slots=50, last=4, taken=1)
+    places = {SPACED[at] + by if by >= 0 else SPACED[at] - 4 * (size[name] - 1),  # its start, or its last element there
+              SPACED[at] + 4 * (size[at] - 1)}                                    # its first element on the other's last
+    for place in places:
+        if by == 4 and size[at] == 1:
+            continue
+        assert L.sparse_attn_page_tables(*dict(SPACED, **{name: place}).values()) == INV, hex(place)
