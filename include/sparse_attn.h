@@ -476,8 +476,9 @@ int sparse_attn_paged_store(int64_t tokens, int32_t kv_heads, int32_t d_head, in
  *   table_stride  0: one row for the whole batch;  max_pos < max_pages * page
  * Entries of the table that hold no attended position are not read; one that does and is no page of
  * the pool makes the row's o and lse NaN.  q . k, the softmax and the sums are in fp32; bf16 weights
- * enter the product with V with 16 bits.  A NaN or an infinity among a row's own keys and values
- * makes what depends on it NaN or infinite; other rows of the cache are never read into a result.
+ * enter the product with V with 16 bits.  A score of -inf (an infinite key, or a product beyond fp32) has the
+ * weight 0, and a row that has no other is as one without a key; any other infinity or NaN among a row's own keys
+ * and values makes what depends on it NaN or infinite; other rows of the cache are never read into a result.
  * batch * heads < 2^22, else SA_ERR_UNSUPPORTED.
  */
 int sparse_attn_paged_decode_workspace_size(int64_t max_pos, int32_t stride_l, int32_t summary_c, int32_t pattern,
@@ -508,7 +509,8 @@ int sparse_attn_paged_decode(const int32_t* positions, int64_t max_pos, int32_t 
  *   lse      device output [heads, tokens] contiguous fp32: natural log, -inf (and o = 0) for an empty set
  * Any length, also 1, and any stride: n is no multiple of anything.  l >= the longest sequence with
  * SA_STRIDED, SA_MODE_A1 is dense causal attention.  Precision as sparse_attn_fwd (bf16 weights are
- * rounded once for the product with V).  An infinity or a NaN reaches the rows that attend it alone.
+ * rounded once for the product with V).  An infinity or a NaN reaches the rows that attend it alone; a score of
+ * -inf has the weight 0, and a row that has no other is as one with an empty set.
  * Addresses 16-byte aligned (starts and lse 4), strides multiples of 16 bytes.
  * workspace: sparse_attn_packed_workspace_size bytes (0 but for strided merged heads with 2 l <
  * tokens), 16-byte aligned, contents ignored; calls that share one must not overlap.

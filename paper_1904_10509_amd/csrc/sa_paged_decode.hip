@@ -359,12 +359,14 @@ paged_split_kernel(PagedArgs a, const T* __restrict__ q, float* __restrict__ par
                 for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
             m = mx;
         }
+        // while every score so far is -inf, m is too: 0 as reference gives them the weight 0 that they have elsewhere
+        const float m_ref = m == -INFINITY ? 0.f : m;
         // (the difference first: scaling before would lose 2^-24 of the scores themselves)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[t][i] = exp2_fast((s[t][i] - m) * a.scale_log2);
+                s[t][i] = exp2_fast((s[t][i] - m_ref) * a.scale_log2);
                 l += s[t][i];
             }
         add_values<D>(mine.rows, s, g, r, acc, T{});
