@@ -61,23 +61,37 @@ struct TilePlace {
     int32_t base, n, i0;
 };
 
-// Every wave finds the sequence of a place by itself: 64 candidates a round, all loads of a round at once.
+// The last sequence whose places begin at `place` or before.  Every wave finds it by itself.  More than 128 sequences
+// are cut into 64 runs, whose first ones a round compares, until a run has no more; those are compared 64 a round, all
+// loads of a round at once, up to the first that begins behind the place.  2^20 sequences take four rounds.  (8,000
+// prompts of one token, 8 heads of 64, bf16: 1,545 us with 64 after 64 from the first one on, 402 so.)
 struct Found {
     int32_t s, start, end;  // s < 0: none
 };
 __device__ inline Found sequence_of(const PackedArgs& a, uint32_t rows, uint32_t place, int lane) {
+    auto clamped = [&](int32_t s) { return max(0, min(a.starts[s], a.tokens)); };
+    auto first_place = [&](int32_t s, int32_t start) { return a.by_rows ? (uint32_t)start : (uint32_t)start / rows + s; };
+    int32_t lo = 0, hi = a.sequences;
+    while (hi - lo > 128) {
+        const int32_t run = (hi - lo + 63) / 64, s = lo + lane * run;
+        const bool below = s < hi && first_place(s, clamped(s)) <= place;
+        const int found = __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));  // (places ascend with s)
+        if (found == 0) return {-1, 0, 0};
+        lo += (found - 1) * run;
+        hi = min(hi, lo + run);
+    }
     Found f{-1, 0, 0};
-    for (int s0 = 0; s0 < a.sequences; s0 += 64) {
-        const int s = s0 + lane;
+    for (int32_t s0 = lo; s0 < hi; s0 += 64) {
+        const int32_t s = s0 + lane;
         int32_t start = 0, end = 0;
         bool below = false;
-        if (s < a.sequences) {
-            start = max(0, min(a.starts[s], a.tokens));
-            end = max(0, min(a.starts[s + 1], a.tokens));
-            below = a.by_rows ? (uint32_t)start <= place : (uint32_t)start / rows + s <= place;
+        if (s < hi) {
+            start = clamped(s);
+            end = clamped(s + 1);
+            below = first_place(s, start) <= place;
         }
         const uint64_t m = __builtin_amdgcn_ballot_w64(below);
-        const int found = __builtin_popcountll(m);  // (places begin in the order of the sequences)
+        const int found = __builtin_popcountll(m);
         if (found > 0) {
             f.s = s0 + found - 1;
             f.start = __builtin_amdgcn_readlane(start, found - 1);
