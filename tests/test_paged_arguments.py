@@ -124,3 +124,17 @@ def test_refusals(library, call, over):
     with pytest.raises(ValueError):
         call(**over)
     assert not library.calls
+
+
+def test_every_written_tensor_is_reported(library):
+    """Each of a call's given outputs by itself: a graph that saved one of them has to know."""
+    table, out, lse = ints(B, 4), gpu(N, H, D), gpu(H, N, dtype=torch.float32)
+    m = sa.PageMap(ints(B + 1), ints(N), ints(N), ints(B), ints(1))
+    step_out, step_lse = gpu(B, H, D), gpu(B, H, dtype=torch.float32)
+    written = [table, m.starts, m.positions, m.slots, m.last, m.taken, out, lse, step_out, step_lse]
+    before = [t._version for t in written]
+    assert tables(table=table, out=m) is m
+    packed(out=out, lse=lse)
+    decode(out=step_out, lse=step_lse)
+    for i, (t, version) in enumerate(zip(written, before)):
+        assert t._version > version, i
