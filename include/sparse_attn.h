@@ -505,7 +505,7 @@ int sparse_attn_paged_decode(const int32_t* positions, int64_t max_pos, int32_t 
  *            attends the set of head h
  *   q, o     [tokens, heads, d_head], k, v [tokens, kv_heads, d_head] of type dtype, element strides
  *            [0..1] (token, head) of their own, d contiguous (q, k and v may be parts of one tensor);
- *            o's rows must not overlap, nor lie in the inputs
+ *            o's rows must not overlap, nor lie in the inputs (o = k or o = v: SA_ERR_INVALID)
  *   lse      device output [heads, tokens] contiguous fp32: natural log, -inf (and o = 0) for an empty set
  * Any length, also 1, and any stride: n is no multiple of anything.  l >= the longest sequence with
  * SA_STRIDED, SA_MODE_A1 is dense causal attention.  Precision as sparse_attn_fwd (bf16 weights are

@@ -1029,6 +1029,7 @@ int sparse_attn_packed_fwd(int32_t sequences, const int32_t* starts, int64_t tok
     const size_t need = sa::packed_workspace_bytes(tokens, p.pattern, head_mode, stride_l, heads, d_head);
     if (workspace_bytes < need) return SA_ERR_BUFFER_TOO_SMALL;
     if (need > 0 && (!workspace || !aligned16(workspace))) return SA_ERR_INVALID;
+    if (o == k || o == v) return SA_ERR_INVALID;  // rows would be written while others still read them
     p.starts = starts;
     p.q = q, p.k = k, p.v = v, p.o = o;
     p.qt = q_strides[0], p.qh = q_strides[1];

@@ -980,7 +980,8 @@ def packed_forward(q, k, v, starts, stride_l, summary_c, pattern, head_mode, sof
     """O [tokens, h, d] and LSE [h, tokens] of sparse attention over sequences packed one behind the other: q [tokens, h,
     d], k and v [tokens, kv_h, d], sequence s in rows starts[s] .. starts[s + 1] - 1 (int32 [sequences + 1] on the
     device).  ``stride_l`` from the longest sequence on with SA_STRIDED and SA_MODE_A1 is dense causal attention.  Rows
-    outside all sequences are left as they were in ``out`` and ``lse``.  The result is not differentiable."""
+    outside all sequences are left as they were in ``out`` and ``lse``; ``out`` must not lie in the inputs.  The result is
+    not differentiable."""
     shape, device, dtype = q.shape, q.device, q.dtype
     k_shape, q_st, k_st, v_st = k.shape, q.stride(), k.stride(), v.stride()
     if len(shape) != 3 or len(k_shape) != 3 or v.shape != k_shape or k_shape[0] != shape[0] or k_shape[2] != shape[2]:

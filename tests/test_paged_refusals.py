@@ -145,3 +145,10 @@ def test_page_tables_that_overlap(L, name, at, by):
         if by == 4 and size[at] == 1:
             continue
         assert L.sparse_attn_page_tables(*dict(SPACED, **{name: place}).values()) == INV, hex(place)
+
+
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("mode", [sa.SA_MODE_MERGED, sa.SA_MODE_A1])
+def test_packed_output_in_an_input(L, which, mode):
+    args = dict(PACKED, mode=mode, q=0x300000, k=0x400000, v=0x500000, o=0x200000)
+    assert L.sparse_attn_packed_fwd(*dict(args, **{which: args["o"]}).values()) == INV
