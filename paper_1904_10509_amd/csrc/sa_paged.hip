@@ -149,35 +149,21 @@ __global__ void __launch_bounds__(kTableThreads) page_tables_kernel(PageTables a
 constexpr int kStoreThreads = 256;
 constexpr int64_t kMaxStoreGroups = 1 << 22;
 
-// Piece n of the call: 16 bytes of one row, pieces fastest, then heads, then tokens.  A thread moves N of
-// K and V each.
-template <int N>
+// Piece n of the call: 16 bytes of one row of K and of V, pieces fastest, then heads, then tokens.
 __global__ void __launch_bounds__(kStoreThreads) paged_store_kernel(PagedStore a) {
     const int64_t total = a.tokens * a.heads << a.piece_shift;
-    const int64_t each = (int64_t)gridDim.x * (kStoreThreads * N);
-    for (int64_t n0 = (int64_t)blockIdx.x * (kStoreThreads * N) + threadIdx.x; n0 < total; n0 += each) {
-        u32x4 k[N], v[N];
-        int64_t to[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int64_t n = n0 + i * kStoreThreads;
-            to[i] = -1;
-            if (n >= total) continue;
-            const int64_t row = n >> a.piece_shift, piece = n & ((1 << a.piece_shift) - 1);
-            const int64_t t = row / a.heads, h = row - t * a.heads;
-            const int32_t slot = a.slots[t];
-            const int32_t page = slot >> a.shift;
-            if (slot < 0 || page >= a.pages) continue;
-            k[i] = *reinterpret_cast<const u32x4*>(a.k + t * a.kt + h * a.kh + piece * 16);
-            v[i] = *reinterpret_cast<const u32x4*>(a.v + t * a.vt + h * a.vh + piece * 16);
-            to[i] = page * a.cache.sp + h * a.cache.sh + (slot & ((1 << a.shift) - 1)) * a.cache.st + piece * 16;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (to[i] < 0) continue;
-            *reinterpret_cast<u32x4*>(a.cache.k + to[i]) = k[i];
-            *reinterpret_cast<u32x4*>(a.cache.v + to[i]) = v[i];
-        }
+    const int64_t each = (int64_t)gridDim.x * kStoreThreads;
+    for (int64_t n = (int64_t)blockIdx.x * kStoreThreads + threadIdx.x; n < total; n += each) {
+        const int64_t row = n >> a.piece_shift, piece = n & ((1 << a.piece_shift) - 1);
+        const int64_t t = row / a.heads, h = row - t * a.heads;
+        const int32_t slot = a.slots[t];
+        const int32_t page = slot >> a.shift;
+        if (slot < 0 || page >= a.pages) continue;
+        const u32x4 k = *reinterpret_cast<const u32x4*>(a.k + t * a.kt + h * a.kh + piece * 16);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(a.v + t * a.vt + h * a.vh + piece * 16);
+        const int64_t to = page * a.cache.sp + h * a.cache.sh + (slot & ((1 << a.shift) - 1)) * a.cache.st + piece * 16;
+        *reinterpret_cast<u32x4*>(a.cache.k + to) = k;
+        *reinterpret_cast<u32x4*>(a.cache.v + to) = v;
     }
 }
 
@@ -193,7 +179,7 @@ hipError_t page_tables_launch(const PageTables& a, hipStream_t stream) {
 hipError_t paged_store_launch(const PagedStore& a, hipStream_t stream) {
     const int64_t total = a.tokens * a.heads << a.piece_shift;
     const int64_t groups = max64(1, min64((total + kStoreThreads - 1) / kStoreThreads, kMaxStoreGroups));
-    hipLaunchKernelGGL(paged_store_kernel<1>, dim3((unsigned)groups), dim3(kStoreThreads), 0, stream, a);
+    hipLaunchKernelGGL(paged_store_kernel, dim3((unsigned)groups), dim3(kStoreThreads), 0, stream, a);
     return hipGetLastError();
 }
 
