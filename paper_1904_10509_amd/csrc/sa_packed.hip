@@ -19,8 +19,9 @@
 // empty.
 //
 // What bounds it: long walks the matrix products and the exponentials beside them, which share a SIMD's time (32
-// heads of 128, 4 x 4,096 dense: 680 us, 809 TFLOP/s; products 36%, vector instructions 43% of it), short ones the
-// steps' latency and, strided merged, the states' way through memory.
+// heads of 128, 4 x 4,096 dense: 680-694 us, 792-809 TFLOP/s; by the counters the products keep a SIMD busy for 40% of
+// it and vector instructions issue for 46%; heads of 64, 65,536 fixed: 37% and 68%), short ones the steps' latency (two
+// sequences of 12,288, strided merged: waves wait 53% of their time) and, strided merged, the states' way through memory.
 #include "sa_finite.h"
 #include "sa_internal.h"
 #include "sa_mask.h"
@@ -422,7 +423,10 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
         for (int x = 0; x < KS; ++x) qf[x] = ld_bf16x8(p + 16 * x + 8 * hh);
     }
     begin();
-    // (no load that the compiler tracks is left inside the loop: a wait for one would drain the ring)
+    // (no load is left inside the loop: a wait for one would drain the ring.  Where registers run out the compiler puts
+    // some there all the same: fixed sets at d = 128 have two of the query's operands in scratch and reload them in every
+    // step behind the next step's loads, so that a wave waits for those too.  65,536, 8 heads of 128 on 4, l = 256, c = 32:
+    // 1,361 us, 830 TFLOP/s, waves wait 38% of their time; strided ones, whose scratch is touched outside the loop, 20%)
     wait_loads_upto<0>();
     int e = 0;
     two_stage_while([&](auto stage) {
@@ -507,7 +511,10 @@ packed_bf16_kernel(PackedArgs a, const uint16_t* __restrict__ q, const uint16_t*
                 }
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    // weights rounded to bf16 for the matrix product, 2^-9 of each; the sum takes them whole
+                    // Weights rounded to bf16 for the matrix product, off by up to 2^-8 each; the sum takes them whole.
+                    // The attention over a layout rounds them so too, and the two are to agree.  Two pieces would take
+                    // the error against 64 bits from 0.0019-0.0021 to the output's own rounding, 0.0016, for half as
+                    // many products again (9 prompts dense 579 -> 782 us, audio 1,185 -> 1,651).
                     const bf16x8 pf = pack_half(s[kb], n);
                     bf16x8 vt[DB];
 #pragma unroll
@@ -856,7 +863,10 @@ packed_f32_kernel(PackedArgs a, const float* __restrict__ q, const float* __rest
 // ---------------------------------------------------------------------------
 constexpr int64_t kMaxGridX = 1 << 20;     // workgroups along x; along y the rest
 // Tiles of 128 rows from so many workgroups on, which fill the chip; below, tiles of 64 (d = 128: always 128, as
-// two waves a workgroup would leave its 64 KB of LDS half used).
+// two waves a workgroup would leave its 64 KB of LDS half used).  Heads of 64, us, 128 rows | 64: 2 x 8,192 dense of 16
+// heads 400 | 444, 65,536 + 57,026 fixed 1,175 | 1,345; 2 x 12,288 strided merged of 8 heads 76 | 74, six ragged ones 88 |
+// 78.  The count takes in the places that stay empty, so many short prompts of 8 heads have tiles of 128 rows too, which
+// they fill less: 200 of 20 tokens 16.0 | 11.7, 1,000 of 20 61.5 | 43.3, 100 of 1,000 strided merged 862 | 608.
 constexpr int64_t kWidePlaces = 1024;
 
 dim3 grid_of(const PackedArgs& a) {

@@ -37,7 +37,7 @@ struct PagedArgs {
     int pattern, mode, heads, kv_heads, splits;
     HeadUnits u;
     int32_t sub, max_pos, l, sc;
-    int32_t least;               // keys of a range, at least
+    int32_t least;               // keys that a range is counted for, at least
     int32_t batch;
     int32_t each;                // ranges of every sequence at most; 0: `splits` of the whole batch (share_of)
     int2* cuts;                  // [batch, heads]: first range and ranges of a row
@@ -465,8 +465,12 @@ struct Cut {
 //   rows take 68 KB of LDS, 3 for d = 64, 5 for d = 32), so that they end together (one sequence of 32,768, 4 cache
 //   heads of 128: 21.3 us, twice as many 29.2; 16 sequences of 866 to 32,767: 53.8 | 63.4), or four for each sequence.
 //   More sequences, whose sums every workgroup would form at length: a number for each, four or what leaves a range
-//   2,048 keys within 32,768 workgroups; short ranges even out over several rounds.
-// No range has fewer than 128 keys, one chunk a wave (two of fp32).
+//   2,048 keys within 32,768 workgroups; short ranges even out over several rounds.  Ragged dense batches, us, at least
+//   1 | 2 | 4 | 8 ranges: 96 of up to 4,096 (8 heads of 64) 44.7 | 44.7 | 42.8 | 46.9, 128 of up to 32,768 (32 on 4 of 128) 256 |
+//   257 | 255 | 253, but 512 of up to 1,024 (8 of 64), which fill the chip by themselves, 62.6 | 76.1 | 109 | 140; ranges
+//   of 1,024 | 2,048 | 4,096 keys at four: 128 of up to 32,768 293 | 255 | 257, 80 of up to 65,536 (8 of 64) 289 | 275 | 271.
+// Ranges are counted for 128 keys each at least, one chunk a wave (two of fp32), and then made equal, the last with what
+// is left (129 keys: 65 and 64); a shorter set is one range.
 constexpr int32_t kLeastKeys = 128;
 Cut cut_of(int pattern, int mode, int32_t sub, int32_t max_pos, int32_t l, int32_t c, int64_t batch, int64_t units, int d) {
     const int64_t count = largest_set(pattern, mode, sub, max_pos, l, c);
